@@ -11,6 +11,9 @@
  *      training-plasticity metric of Eq. 1 (SP loss)          (egeria_plasticity)
  * egeria_plasticity_eval chains 2 and 3 for a stack of modules,
  * egeria_refresh_eval chains 1, 2 and 3.
+ * Beside it: the freeze decision, the activation cache, and attention with its
+ * gradient for the training model's Transformer layers (egeria_attention*,
+ * egeria_position_bias*).
  *
  * General rules of this interface
  *   - Every pointer is a DEVICE pointer unless its comment says HOST.  The
@@ -477,6 +480,114 @@ egeria_status egeria_cache_put(const egeria_cache_desc *desc, void *cache, size_
                                const int64_t *ids, int32_t n, const void *rows, void *stream);
 egeria_status egeria_cache_get(const egeria_cache_desc *desc, const void *cache, size_t cache_bytes,
                                const int64_t *ids, int64_t n, void *out, uint8_t *hit, void *stream);
+
+/* ---------------------------------------------------------------------------
+ * Attention of the training model's Transformer layers: the layers whose
+ * activations A_T the score takes and whose weights a snapshot quantises
+ * (Section 4.2; the reference model's own attention is part of
+ * egeria_ref_forward).  Forward, backward, and the learned relative position
+ * bias that both add to the scores.
+ *
+ * For sequence b, head h, query i, key j, with n_q and n_k the sequence's
+ * lengths (q_lens[b], k_lens[b]; without them q_len and k_len), key head
+ * g = h / (heads / kv_heads) and shift = n_k - n_q where causal, else 0:
+ *   visible:  i < n_q, j < n_k, and, where causal, j <= i + shift
+ *             (the ends of the two sequences are aligned: one query is the last
+ *             token of its keys);
+ *   s_ij = scale * <q_i, k_j> + table[bucket(j - i - shift), h]  for visible pairs;
+ *   L_i  = log sum_j exp(s_ij),  p_ij = exp(s_ij - L_i),  o_i = sum_j p_ij v_j.
+ * A row without a visible pair (an empty sequence, a query beyond n_q, a causal
+ * query before the first key) has o = 0 and L = -infinity.  Keys and values at
+ * or beyond n_k, and queries at or beyond n_q, are not read; a non-finite value
+ * of a visible key may reach every query of its sequence, as in any product.
+ * Backward, from dout = dLoss/do:
+ *   D_i = <dout_i, o_i>,  ds_ij = p_ij (<dout_i, v_j> - D_i)
+ *   dq_i = scale sum_j ds_ij k_j,  dk_j = scale sum_{i, h of group g} ds_ij q_i,
+ *   dv_j = sum_{i, h of group g} p_ij dout_i,
+ *   dtable[n, h] = sum over b and the visible i, j of bucket n of ds_ij.
+ * Every element of every output is written: zeros for rows without a visible
+ * pair, for queries at or beyond n_q and for keys at or beyond n_k.
+ *
+ * Scores, row statistics and sums are fp32.  With EGERIA_BF16, p and ds are
+ * rounded to bf16 where they enter the products on the matrix cores, and the
+ * outputs once at the end; with EGERIA_F32 nothing is rounded below fp32.
+ * Results do not depend on timing (no floating-point atomics between waves).
+ * ------------------------------------------------------------------------- */
+
+/* HOST struct.  A learned bias by the relative position of key and query.
+ * bucket(r): with n = buckets / 2 for each side where bidirectional (the keys
+ * after the query, r > 0, have the upper half of the rows), else n = buckets for
+ * the keys up to the query (all later keys count as r = 0); distance |r|;
+ * e = n / 2, m = n - e: a distance below e is a bucket of its own, bucket e + k
+ * begins at the smallest whole distance >= e (max_distance / e)^(k / m), and the
+ * last bucket has no end.  Limits: buckets <= 128, even and at least 4 where
+ * bidirectional, at least 2 otherwise; n / 2 < max_distance <= 1024.
+ * In the attention calls an entry of -1e30 or less (minus infinity, the lowest
+ * value of a type) hides its pairs. */
+typedef struct {
+    const float *table;             /* DEVICE fp32 [buckets, heads] */
+    int32_t buckets;
+    int32_t max_distance;
+    int32_t bidirectional;
+} egeria_position_table;
+
+/* HOST struct.  A DEVICE tensor [batch, token, head, head_dim] of the call's
+ * dtype whose features are contiguous; strides in elements, not negative.  The
+ * data pointer needs the alignment of its type only (16 bytes, with strides in
+ * whole units of 16 bytes and head_dim * size a multiple of 16, is faster).
+ * Strides of inputs may be 0; elements of outputs must not overlap. */
+typedef struct {
+    void *data;
+    int64_t batch_stride, token_stride, head_stride;
+} egeria_heads;
+
+/* HOST struct.  One attention call's sizes. */
+typedef struct {
+    int32_t dtype;                  /* egeria_dtype of q, k, v, out and the gradients */
+    int32_t batch, heads, kv_heads; /* kv_heads divides heads */
+    int32_t q_len, k_len, head_dim; /* head_dim <= 128 */
+    int32_t causal;
+    float scale;
+    const int32_t *q_lens, *k_lens; /* DEVICE int32 [batch] or NULL; values are clamped to [0, q_len] and [0, k_len] */
+    const egeria_position_table *bias;  /* HOST, or NULL */
+} egeria_attention_desc;
+
+/* Host-only and pure: bytes of workspace egeria_attention (backward = 0) or
+ * egeria_attention_backward (backward = 1) need; 0 if desc is invalid. */
+size_t egeria_attention_workspace_bytes(const egeria_attention_desc *desc, int32_t backward);
+
+/* out: [batch, q_len, heads, head_dim].  lse: fp32 [batch, heads, q_len], L of every row.
+ * Errors: EGERIA_ERR_INVALID_ARG for a bad descriptor or table, a null or
+ * misaligned pointer, a negative stride, an output whose elements overlap;
+ * EGERIA_ERR_UNSUPPORTED for head_dim > 128 or sizes beyond 2^31 workgroups or
+ * 2^62 bytes; EGERIA_ERR_WORKSPACE_TOO_SMALL. */
+egeria_status egeria_attention(const egeria_attention_desc *desc, const egeria_heads *q, const egeria_heads *k,
+                               const egeria_heads *v, const egeria_heads *out, float *lse, void *ws, size_t ws_bytes,
+                               void *stream);
+
+/* out, lse: what egeria_attention wrote.  dtable: fp32 [buckets, heads] out, or
+ * NULL (no gradient of the table; must be NULL without desc->bias).  Errors as above. */
+egeria_status egeria_attention_backward(const egeria_attention_desc *desc, const egeria_heads *dout, const egeria_heads *q,
+                                        const egeria_heads *k, const egeria_heads *v, const egeria_heads *out,
+                                        const float *lse, const egeria_heads *dq, const egeria_heads *dk,
+                                        const egeria_heads *dv, float *dtable, void *ws, size_t ws_bytes, void *stream);
+
+/* The bias as a tensor, for attention that is not computed here:
+ * bias[h, i, j] = table[bucket(j - i - offset), h], rounded once to dt;
+ * bias [heads, q_len, k_len] out, offset the position of query 0 among the keys.
+ * |offset|, q_len, k_len <= 2^29, heads <= 65535. */
+egeria_status egeria_position_bias(const egeria_position_table *t, int32_t heads, int32_t q_len, int32_t k_len, int32_t offset,
+                                   void *bias, egeria_dtype dt, void *stream);
+
+/* The gradient of the table from that of the bias, summed over the batch it was
+ * broadcast over: dbias [batch, heads, q_len, k_len] of type dt, dtable fp32
+ * [buckets, heads] out.  ws: at least egeria_position_bias_workspace_bytes(...)
+ * bytes (0: invalid arguments).  t->table is not read, but must be set. */
+egeria_status egeria_position_bias_backward(const egeria_position_table *t, const void *dbias, egeria_dtype dt, int32_t batch,
+                                            int32_t heads, int32_t q_len, int32_t k_len, int32_t offset, float *dtable,
+                                            void *ws, size_t ws_bytes, void *stream);
+size_t egeria_position_bias_workspace_bytes(const egeria_position_table *t, int32_t batch, int32_t heads, int32_t q_len,
+                                            int32_t k_len, egeria_dtype dt);
 
 #ifdef __cplusplus
 }

@@ -7,7 +7,8 @@ import subprocess
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libegeria.so")
-SOURCES = ["api.hip", "quantize.hip", "gemm_i8.hip", "gram.hip", "bert.hip", "freeze.hip", "cache.hip", "cast.hip", "affine.hip", "microbench.hip"]
+SOURCES = ["api.hip", "quantize.hip", "gemm_i8.hip", "gram.hip", "bert.hip", "freeze.hip", "cache.hip", "cast.hip", "affine.hip", "microbench.hip",
+           "attention.hip", "position.hip"]
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 
 FLAGS = [
@@ -26,14 +27,17 @@ def sources():
     return [os.path.join(CSRC, s) for s in SOURCES]
 
 
+def headers():
+    include = os.path.join(os.path.dirname(HERE), "include")
+    return ([os.path.join(include, h) for h in ("egeria.h", "egeria_profile.h")] +
+            [os.path.join(CSRC, h) for h in ("common.hpp", "position.hpp", "gelu.hpp", "gelu_table.inc", "gelu_lines.inc")])
+
+
 def is_stale() -> bool:
     if not os.path.exists(LIB):
         return True
     t = os.path.getmtime(LIB)
-    deps = sources() + [os.path.join(CSRC, "common.hpp"),
-                        os.path.join(os.path.dirname(HERE), "include", "egeria.h"),
-                        os.path.join(os.path.dirname(HERE), "include", "egeria_profile.h"), os.path.join(CSRC, "gelu.hpp"), os.path.join(CSRC, "gelu_table.inc"),
-               os.path.join(CSRC, "gelu_lines.inc")]
+    deps = sources() + headers()
     return any(os.path.getmtime(d) > t for d in deps)
 
 
@@ -54,12 +58,9 @@ def build_library(force: bool = True) -> str:
     os.makedirs(objdir, exist_ok=True)
     compile_flags = [f for f in FLAGS if f != "-shared"]
     jobs = []
-    headers = [os.path.join(CSRC, "common.hpp"), os.path.join(os.path.dirname(HERE), "include", "egeria.h"),
-               os.path.join(os.path.dirname(HERE), "include", "egeria_profile.h"), os.path.join(CSRC, "gelu.hpp"), os.path.join(CSRC, "gelu_table.inc"),
-               os.path.join(CSRC, "gelu_lines.inc")]
     for src in sources():
         obj = os.path.join(objdir, os.path.basename(src) + ".o")
-        fresh = os.path.exists(obj) and all(os.path.getmtime(d) <= os.path.getmtime(obj) for d in [src] + headers)
+        fresh = os.path.exists(obj) and all(os.path.getmtime(d) <= os.path.getmtime(obj) for d in [src] + headers())
         jobs.append(([HIPCC] + compile_flags + ["-c", src, "-o", obj], obj, force or not fresh))
     with ThreadPoolExecutor(max_workers=min(8, len(jobs))) as pool:
         list(pool.map(lambda j: _run(j[0]) if j[2] else None, jobs))

@@ -88,6 +88,20 @@ class CacheDesc(ctypes.Structure):
     _fields_ = [("window", _i32), ("batch", _i32), ("row_elems", _i64), ("dtype", _i32)]
 
 
+class PositionTable(ctypes.Structure):
+    _fields_ = [("table", _vp), ("buckets", _i32), ("max_distance", _i32), ("bidirectional", _i32)]
+
+
+class Heads(ctypes.Structure):
+    _fields_ = [("data", _vp), ("batch_stride", _i64), ("token_stride", _i64), ("head_stride", _i64)]
+
+
+class AttentionDesc(ctypes.Structure):
+    _fields_ = [("dtype", _i32), ("batch", _i32), ("heads", _i32), ("kv_heads", _i32), ("q_len", _i32), ("k_len", _i32),
+                ("head_dim", _i32), ("causal", _i32), ("scale", ctypes.c_float), ("q_lens", _vp), ("k_lens", _vp),
+                ("bias", ctypes.POINTER(PositionTable))]
+
+
 class EgeriaError(RuntimeError):
     def __init__(self, code: int, where: str):
         self.code = code
@@ -107,6 +121,8 @@ EXPORTS = [
     "egeria_refresh_eval", "egeria_plasticity_noalloc", "egeria_profile_attention", "egeria_profile_attention_bounds",
     "egeria_quantize_affine", "egeria_quantize_affine_workspace_bytes", "egeria_microbench",
     "egeria_profile_attention_threshold", "egeria_profile_attention_certified", "egeria_profile_gemm_tile", "egeria_profile_gemm_stages",
+    "egeria_attention", "egeria_attention_backward", "egeria_attention_workspace_bytes", "egeria_position_bias",
+    "egeria_position_bias_backward", "egeria_position_bias_workspace_bytes",
 ]
 
 (KERNEL_NONE, KERNEL_ABSMAX, KERNEL_QUANTIZE, KERNEL_GEMM, KERNEL_GRAM, KERNEL_ATTENTION, KERNEL_LAYERNORM,
@@ -201,6 +217,20 @@ def lib():
     L.egeria_cache_put.argtypes = [ctypes.POINTER(CacheDesc), _vp, _sz, _vp, _i32, _vp, _vp]
     L.egeria_cache_get.restype = ctypes.c_int
     L.egeria_cache_get.argtypes = [ctypes.POINTER(CacheDesc), _vp, _sz, _vp, _i64, _vp, _vp, _vp]
+    L.egeria_attention_workspace_bytes.restype = _sz
+    L.egeria_attention_workspace_bytes.argtypes = [ctypes.POINTER(AttentionDesc), _i32]
+    L.egeria_attention.restype = ctypes.c_int
+    L.egeria_attention.argtypes = [ctypes.POINTER(AttentionDesc)] + [ctypes.POINTER(Heads)] * 4 + [_vp, _vp, _sz, _vp]
+    L.egeria_attention_backward.restype = ctypes.c_int
+    L.egeria_attention_backward.argtypes = ([ctypes.POINTER(AttentionDesc)] + [ctypes.POINTER(Heads)] * 5 + [_vp] +
+                                            [ctypes.POINTER(Heads)] * 3 + [_vp, _vp, _sz, _vp])
+    L.egeria_position_bias.restype = ctypes.c_int
+    L.egeria_position_bias.argtypes = [ctypes.POINTER(PositionTable), _i32, _i32, _i32, _i32, _vp, ctypes.c_int, _vp]
+    L.egeria_position_bias_backward.restype = ctypes.c_int
+    L.egeria_position_bias_backward.argtypes = [ctypes.POINTER(PositionTable), _vp, ctypes.c_int, _i32, _i32, _i32, _i32, _i32,
+                                                _vp, _vp, _sz, _vp]
+    L.egeria_position_bias_workspace_bytes.restype = _sz
+    L.egeria_position_bias_workspace_bytes.argtypes = [ctypes.POINTER(PositionTable), _i32, _i32, _i32, _i32, ctypes.c_int]
     L.egeria_status_string.restype = ctypes.c_char_p
     L.egeria_status_string.argtypes = [ctypes.c_int]
     _lib = L
@@ -668,6 +698,147 @@ class ActivationCache:
                                       _ptr(_dev(ids)) if n else None, n, _ptr(_dev(out)) if n else None,
                                       _ptr(hit) if n else None, _stream()), "egeria_cache_get")
         return hit
+
+
+# ---- attention of the training model -----------------------------------------------------------
+
+class PositionBias(NamedTuple):
+    """A learned bias by relative position: table fp32 [buckets, heads] (egeria_position_table)."""
+    table: torch.Tensor
+    max_distance: int
+    bidirectional: bool = True
+
+    def c_struct(self) -> PositionTable:
+        t = _dev(self.table)
+        if t.dtype != torch.float32 or t.dim() != 2:
+            raise ValueError("a position table is fp32 [buckets, heads]")
+        return PositionTable(t.data_ptr(), t.shape[0], int(self.max_distance), 1 if self.bidirectional else 0)
+
+
+def _same_device(*tensors: Optional[torch.Tensor]) -> None:
+    """Kernels go to the current device's current stream: everything a call touches has to be there."""
+    here = torch.cuda.current_device() if any(t is not None and t.is_cuda for t in tensors) else -1
+    for t in tensors:
+        if t is not None and (not t.is_cuda or t.device.index != here):
+            raise ValueError("tensors on the current device expected")
+
+
+def _heads(t: torch.Tensor) -> Heads:
+    if t.dim() != 4:
+        raise ValueError("[batch, token, head, feature] expected")
+    if t.shape[3] > 1 and t.stride(3) != 1:
+        raise ValueError("contiguous features expected")
+    return Heads(t.data_ptr(), t.stride(0), t.stride(1), t.stride(2))
+
+
+def _lens(t: Optional[torch.Tensor], batch: int):
+    if t is None:
+        return None
+    if t.dtype != torch.int32 or t.shape != (batch,) or not t.is_contiguous():
+        raise ValueError("lengths are a contiguous int32 tensor [batch]")
+    return t.data_ptr()
+
+
+def _attention_desc(q, k, v, causal, scale, q_lens, k_lens, bias) -> AttentionDesc:
+    if q.dim() != 4 or k.dim() != 4 or k.shape != v.shape or k.shape[0] != q.shape[0] or k.shape[3] != q.shape[3]:
+        raise ValueError("q [batch, q_len, heads, dim] and k, v [batch, k_len, kv_heads, dim] expected")
+    if not q.dtype == k.dtype == v.dtype:
+        raise ValueError("q, k and v must have one dtype")
+    batch, q_len, heads, dim = q.shape
+    tab = None
+    if bias is not None:
+        if bias.table.dim() != 2 or bias.table.shape[1] != heads:
+            raise ValueError("a position table is fp32 [buckets, heads]")
+        tab = ctypes.pointer(bias.c_struct())
+    scale = 1.0 / math.sqrt(dim) if scale is None and dim else scale
+    return AttentionDesc(_dt(q), batch, heads, k.shape[2], q_len, k.shape[1], dim, 1 if causal else 0, scale or 0.0,
+                         _lens(q_lens, batch), _lens(k_lens, batch), tab)
+
+
+def attention_workspace_bytes(desc: AttentionDesc, backward: bool) -> int:
+    return int(lib().egeria_attention_workspace_bytes(ctypes.byref(desc), 1 if backward else 0))
+
+
+def attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, causal: bool = False, scale: Optional[float] = None,
+              q_lens: Optional[torch.Tensor] = None, k_lens: Optional[torch.Tensor] = None,
+              bias: Optional[PositionBias] = None, out: Optional[torch.Tensor] = None, lse: Optional[torch.Tensor] = None,
+              ws: Optional[torch.Tensor] = None):
+    """egeria_attention: q [batch, q_len, heads, dim], k and v [batch, k_len, kv_heads, dim] (any strides with contiguous
+    features) -> out like q, and lse fp32 [batch, heads, q_len].  scale: 1 / sqrt(dim) if not given."""
+    _same_device(q, k, v, q_lens, k_lens, out, lse, ws, None if bias is None else bias.table)
+    desc = _attention_desc(q, k, v, causal, scale, q_lens, k_lens, bias)
+    if out is None:
+        out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+    elif out.shape != q.shape or out.dtype != q.dtype:
+        raise ValueError("out must have q's shape and dtype")
+    if lse is None:
+        lse = torch.empty((q.shape[0], q.shape[2], q.shape[1]), dtype=torch.float32, device=q.device)
+    elif lse.shape != (q.shape[0], q.shape[2], q.shape[1]) or lse.dtype != torch.float32 or not lse.is_contiguous():
+        raise ValueError("lse must be a contiguous fp32 tensor [batch, heads, q_len]")
+    ws = workspace(attention_workspace_bytes(desc, False), q.device) if ws is None else ws
+    views = [_heads(t) for t in (q, k, v, out)]
+    rc = lib().egeria_attention(desc, *views, _ptr(lse), _ptr(ws), ws.numel(), _stream())
+    _check(rc, "egeria_attention")
+    return out, lse
+
+
+def attention_backward(dout: torch.Tensor, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, out: torch.Tensor, lse: torch.Tensor,
+                       causal: bool = False, scale: Optional[float] = None, q_lens: Optional[torch.Tensor] = None,
+                       k_lens: Optional[torch.Tensor] = None, bias: Optional[PositionBias] = None,
+                       dq: Optional[torch.Tensor] = None, dk: Optional[torch.Tensor] = None, dv: Optional[torch.Tensor] = None,
+                       ws: Optional[torch.Tensor] = None, table_grad: bool = True):
+    """egeria_attention_backward: (dq, dk, dv, dtable) from the arguments and results of attention().  dtable is fp32
+    [buckets, heads], or None without bias or with table_grad = False.  dq, dk, dv: tensors to write, e.g. the slices of a packed
+    gradient."""
+    _same_device(dout, q, k, v, out, lse, q_lens, k_lens, dq, dk, dv, ws, None if bias is None else bias.table)
+    desc = _attention_desc(q, k, v, causal, scale, q_lens, k_lens, bias)
+    for t, name in ((dout, "dout"), (out, "out")):
+        if t.shape != q.shape or t.dtype != q.dtype:
+            raise ValueError(f"{name} must have q's shape and dtype")
+    if lse.shape != (q.shape[0], q.shape[2], q.shape[1]) or lse.dtype != torch.float32 or not lse.is_contiguous():
+        raise ValueError("lse must be a contiguous fp32 tensor [batch, heads, q_len]")
+    grads = []
+    for g, t, name in ((dq, q, "dq"), (dk, k, "dk"), (dv, v, "dv")):
+        if g is not None and (g.shape != t.shape or g.dtype != t.dtype):
+            raise ValueError(f"{name} must have the shape and dtype of what it is the gradient of")
+        grads.append(torch.empty(t.shape, dtype=t.dtype, device=t.device) if g is None else g)
+    dtable = torch.empty_like(bias.table) if bias is not None and table_grad else None
+    ws = workspace(attention_workspace_bytes(desc, True), q.device) if ws is None else ws
+    rc = lib().egeria_attention_backward(desc, *[_heads(t) for t in (dout, q, k, v, out)], _ptr(lse),
+                                         *[_heads(t) for t in grads], _ptr(dtable), _ptr(ws), ws.numel(), _stream())
+    _check(rc, "egeria_attention_backward")
+    return (*grads, dtable)
+
+
+def position_bias(bias: PositionBias, q_len: int, k_len: int, offset: int = 0, dtype: torch.dtype = torch.float32,
+                  out: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """egeria_position_bias: [heads, q_len, k_len] of table entries; offset = position of query 0 among the keys."""
+    _same_device(bias.table, out)
+    tab, heads = bias.c_struct(), bias.table.shape[1]
+    if out is None:
+        out = torch.empty((heads, q_len, k_len), dtype=dtype, device=bias.table.device)
+    elif _dev(out).shape != (heads, q_len, k_len) or out.dtype != dtype:
+        raise ValueError("out must be [heads, q_len, k_len] of dtype")
+    rc = lib().egeria_position_bias(tab, heads, q_len, k_len, int(offset), _ptr(out), _dt(out), _stream())
+    _check(rc, "egeria_position_bias")
+    return out
+
+
+def position_bias_backward(dbias: torch.Tensor, bias: PositionBias, offset: int = 0, ws: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """egeria_position_bias_backward: the gradient [buckets, heads] of bias.table from dbias [batch, heads, q_len, k_len] (or
+    [heads, q_len, k_len])."""
+    _same_device(dbias, bias.table, ws)
+    tab, heads = bias.c_struct(), bias.table.shape[1]
+    if dbias.dim() not in (3, 4) or dbias.shape[-3] != heads:
+        raise ValueError("dbias must be [batch, heads, q_len, k_len]")
+    batch, q_len, k_len = dbias.shape[0] if dbias.dim() == 4 else 1, dbias.shape[-2], dbias.shape[-1]
+    dtable = torch.empty_like(bias.table)
+    if ws is None:
+        ws = workspace(int(lib().egeria_position_bias_workspace_bytes(tab, batch, heads, q_len, k_len, _dt(dbias))), dbias.device)
+    rc = lib().egeria_position_bias_backward(tab, _ptr(_dev(dbias)), _dt(dbias), batch, heads, q_len, k_len, int(offset),
+                                             _ptr(dtable), _ptr(ws), ws.numel(), _stream())
+    _check(rc, "egeria_position_bias_backward")
+    return dtable
 
 
 def profile_attention(qkv: torch.Tensor, heads: int, mode: int):

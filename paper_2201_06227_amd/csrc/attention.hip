@@ -1,0 +1,356 @@
+// Attention of the training model's Transformer layers and its backward pass (include/egeria.h has the definition).
+#include "position.hpp"
+
+namespace egeria {
+
+namespace {
+
+struct View {
+    char *p;
+    int64_t sb, st, sh;                     // in elements
+};
+
+struct AttnArgs {
+    View q, k, v, o, d_o, dq, dk, dv;
+    float *lse;                             // [batch, heads, q_len]
+    float *delta;                           // [batch, heads, q_len], backward
+    float *partials;                        // [heads][batch * row tiles][buckets], backward with a table gradient
+    const int32_t *q_lens, *k_lens;
+    const float *table;                     // null: no bias
+    int32_t table_rows;
+    int32_t batch, heads, kv_heads, group, q_len, k_len, dim, causal;
+    float scale;
+    Buckets b;
+};
+
+template <typename T> __device__ __forceinline__ float load1(const View &v, int64_t off);
+template <> __device__ __forceinline__ float load1<float>(const View &v, int64_t off) { return ((const float *)v.p)[off]; }
+template <> __device__ __forceinline__ float load1<uint16_t>(const View &v, int64_t off) { return bf16_to_f32(((const uint16_t *)v.p)[off]); }
+template <typename T> __device__ __forceinline__ void store1(const View &v, int64_t off, float x);
+template <> __device__ __forceinline__ void store1<float>(const View &v, int64_t off, float x) { ((float *)v.p)[off] = x; }
+template <> __device__ __forceinline__ void store1<uint16_t>(const View &v, int64_t off, float x)
+{
+    ((uint16_t *)v.p)[off] = __builtin_bit_cast(uint16_t, (__bf16)x);
+}
+
+__device__ __forceinline__ int clamped(const int32_t *lens, int b, int most)
+{
+    const int n = lens ? lens[b] : most;
+    return n < 0 ? 0 : (n > most ? most : n);
+}
+
+// score of a pair that the lengths let see; minus infinity where it is hidden
+template <typename T>
+__device__ __forceinline__ float score(const AttnArgs &a, int h, int64_t qo, int64_t ko, int rel)
+{
+    if (a.causal && rel > 0) return -INFINITY;
+    float s = 0.0f;
+    for (int d = 0; d < a.dim; ++d) s = fmaf(load1<T>(a.q, qo + d), load1<T>(a.k, ko + d), s);
+    s *= a.scale;
+    if (a.table) {
+        const float t = a.table[bucket_of_entry(a.b, distance_index(a.b, rel)) * a.heads + h];
+        s = t <= -1e30f ? -INFINITY : s + t;
+    }
+    return s;
+}
+
+constexpr int kTileRows = 64;
+
+// a wave per row
+template <typename T>
+__global__ __launch_bounds__(256) void attention_kernel(AttnArgs a)
+{
+    const int lane = threadIdx.x & 63;
+    const int64_t row = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+    if (row >= (int64_t)a.batch * a.heads * a.q_len) return;
+    const int i = (int)(row % a.q_len), h = (int)(row / a.q_len % a.heads), b = (int)(row / a.q_len / a.heads);
+    const int nq = clamped(a.q_lens, b, a.q_len), nk = clamped(a.k_lens, b, a.k_len), shift = a.causal ? nk - nq : 0;
+    const int64_t qo = b * a.q.sb + i * a.q.st + h * a.q.sh;
+    float m = -INFINITY, l = 0.0f, o[2] = {0.0f, 0.0f};
+    for (int j0 = 0; i < nq && j0 < nk; j0 += 64) {
+        const int j = j0 + lane;
+        const float s = j < nk ? score<T>(a, h, qo, b * a.k.sb + j * a.k.st + h / a.group * a.k.sh, j - i - shift) : -INFINITY;
+        const float top = fmaxf(m, wave_max(s));
+        if (top == -INFINITY) continue;
+        const float keep = __builtin_amdgcn_exp2f((m - top) * 1.44269504f), p = __builtin_amdgcn_exp2f((s - top) * 1.44269504f);
+        l = l * keep + wave_sum(p);
+        m = top;
+        for (int c = 0; c < 2; ++c) o[c] *= keep;
+        for (int e = 0; e < 64 && j0 + e < nk; ++e) {
+            const float w = __shfl(p, e);
+            if (w == 0.0f) continue;
+            const int64_t vo = b * a.v.sb + (j0 + e) * a.v.st + h / a.group * a.v.sh;
+            for (int c = 0; c < 2; ++c)
+                if (lane + 64 * c < a.dim) o[c] = fmaf(w, load1<T>(a.v, vo + lane + 64 * c), o[c]);
+        }
+    }
+    for (int c = 0; c < 2; ++c)
+        if (lane + 64 * c < a.dim) store1<T>(a.o, b * a.o.sb + i * a.o.st + h * a.o.sh + lane + 64 * c, l > 0.0f ? o[c] / l : 0.0f);
+    if (lane == 0) a.lse[row] = l > 0.0f ? m + logf(l) : -INFINITY;
+}
+
+// p and ds of a pair
+template <typename T>
+__device__ __forceinline__ float pair_grad(const AttnArgs &a, int h, int64_t qo, int64_t oo, int64_t ko, int64_t vo, int rel, float lse, float delta, float *p)
+{
+    const float s = score<T>(a, h, qo, ko, rel);
+    *p = s == -INFINITY || lse == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f((s - lse) * 1.44269504f);
+    float dp = 0.0f;
+    for (int d = 0; d < a.dim; ++d) dp = fmaf(load1<T>(a.d_o, oo + d), load1<T>(a.v, vo + d), dp);
+    return *p == 0.0f ? 0.0f : *p * (dp - delta);
+}
+
+// dq, delta and the partial sums of the table's gradient: kTileRows queries per workgroup, a wave per row
+template <typename T>
+__global__ __launch_bounds__(256) void attention_dq_kernel(AttnArgs a)
+{
+    __shared__ float sums[4][kMaxBuckets];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int tiles = (a.q_len + kTileRows - 1) / kTileRows, tile = blockIdx.x % tiles;
+    const int h = blockIdx.x / tiles % a.heads, b = blockIdx.x / tiles / a.heads;
+    const int nq = clamped(a.q_lens, b, a.q_len), nk = clamped(a.k_lens, b, a.k_len), shift = a.causal ? nk - nq : 0;
+    float acc[2] = {0.0f, 0.0f};
+    for (int i = tile * kTileRows + wave; i < (tile + 1) * kTileRows && i < a.q_len; i += 4) {
+        const int64_t qo = b * a.q.sb + i * a.q.st + h * a.q.sh, oo = b * a.d_o.sb + i * a.d_o.st + h * a.d_o.sh;
+        const int64_t uo = b * a.o.sb + i * a.o.st + h * a.o.sh, row = ((int64_t)b * a.heads + h) * a.q_len + i;
+        float o[2] = {0.0f, 0.0f}, delta = 0.0f;
+        if (i < nq) {
+            for (int d = lane; d < a.dim; d += 64) delta = fmaf(load1<T>(a.d_o, oo + d), load1<T>(a.o, uo + d), delta);
+            delta = wave_sum(delta);
+            const float lse = a.lse[row];
+            for (int j0 = 0; j0 < nk; j0 += 64) {
+                const int j = j0 + lane, rel = j - i - shift;
+                float p = 0.0f, ds = 0.0f;
+                if (j < nk)
+                    ds = pair_grad<T>(a, h, qo, oo, b * a.k.sb + j * a.k.st + h / a.group * a.k.sh,
+                                      b * a.v.sb + j * a.v.st + h / a.group * a.v.sh, rel, lse, delta, &p);
+                const int bucket = a.table ? bucket_of_entry(a.b, distance_index(a.b, rel)) : 0;
+                for (int e = 0; e < 64 && j0 + e < nk; ++e) {
+                    const float w = __shfl(ds, e);
+                    if (a.partials) {
+                        const int n = __shfl(bucket, e);
+                        if (lane == (n & 63)) acc[n >> 6] += w;
+                    }
+                    if (w == 0.0f) continue;
+                    const int64_t ko = b * a.k.sb + (j0 + e) * a.k.st + h / a.group * a.k.sh;
+                    for (int c = 0; c < 2; ++c)
+                        if (lane + 64 * c < a.dim) o[c] = fmaf(w, load1<T>(a.k, ko + lane + 64 * c), o[c]);
+                }
+            }
+        }
+        if (lane == 0) a.delta[row] = delta;
+        for (int c = 0; c < 2; ++c)
+            if (lane + 64 * c < a.dim) store1<T>(a.dq, b * a.dq.sb + i * a.dq.st + h * a.dq.sh + lane + 64 * c, o[c] * a.scale);
+    }
+    if (a.partials) {
+        sums[wave][lane] = acc[0];
+        sums[wave][lane + 64] = acc[1];
+        __syncthreads();
+        for (int n = threadIdx.x; n < a.table_rows; n += 256)
+            a.partials[((int64_t)h * a.batch * tiles + (int64_t)b * tiles + tile) * a.table_rows + n] =
+                (sums[0][n] + sums[1][n]) + (sums[2][n] + sums[3][n]);
+    }
+}
+
+// dk and dv: a wave per key
+template <typename T>
+__global__ __launch_bounds__(256) void attention_dkv_kernel(AttnArgs a)
+{
+    const int lane = threadIdx.x & 63;
+    const int64_t row = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+    if (row >= (int64_t)a.batch * a.kv_heads * a.k_len) return;
+    const int j = (int)(row % a.k_len), g = (int)(row / a.k_len % a.kv_heads), b = (int)(row / a.k_len / a.kv_heads);
+    const int nq = clamped(a.q_lens, b, a.q_len), nk = clamped(a.k_lens, b, a.k_len), shift = a.causal ? nk - nq : 0;
+    float dk[2] = {0.0f, 0.0f}, dv[2] = {0.0f, 0.0f};
+    const int64_t ko = b * a.k.sb + j * a.k.st + g * a.k.sh, vo = b * a.v.sb + j * a.v.st + g * a.v.sh;
+    for (int h = g * a.group; j < nk && h < (g + 1) * a.group; ++h)
+        for (int i0 = 0; i0 < nq; i0 += 64) {
+            const int i = i0 + lane;
+            float p = 0.0f, ds = 0.0f;
+            if (i < nq) {
+                const int64_t at = ((int64_t)b * a.heads + h) * a.q_len + i;
+                ds = pair_grad<T>(a, h, b * a.q.sb + i * a.q.st + h * a.q.sh, b * a.d_o.sb + i * a.d_o.st + h * a.d_o.sh, ko, vo,
+                                  j - i - shift, a.lse[at], a.delta[at], &p);
+            }
+            for (int e = 0; e < 64 && i0 + e < nq; ++e) {
+                const float w = __shfl(ds, e), u = __shfl(p, e);
+                if (u == 0.0f) continue;
+                const int64_t qo = b * a.q.sb + (i0 + e) * a.q.st + h * a.q.sh, oo = b * a.d_o.sb + (i0 + e) * a.d_o.st + h * a.d_o.sh;
+                for (int c = 0; c < 2; ++c)
+                    if (lane + 64 * c < a.dim) {
+                        dk[c] = fmaf(w, load1<T>(a.q, qo + lane + 64 * c), dk[c]);
+                        dv[c] = fmaf(u, load1<T>(a.d_o, oo + lane + 64 * c), dv[c]);
+                    }
+            }
+        }
+    for (int c = 0; c < 2; ++c)
+        if (lane + 64 * c < a.dim) {
+            store1<T>(a.dk, b * a.dk.sb + j * a.dk.st + g * a.dk.sh + lane + 64 * c, dk[c] * a.scale);
+            store1<T>(a.dv, b * a.dv.sb + j * a.dv.st + g * a.dv.sh + lane + 64 * c, dv[c]);
+        }
+}
+
+// ---- host side -------------------------------------------------------------------------------------------------
+
+bool valid_desc(const egeria_attention_desc *d)
+{
+    if (!d || (d->dtype != EGERIA_F32 && d->dtype != EGERIA_BF16)) return false;
+    if (d->batch < 0 || d->heads < 1 || d->kv_heads < 1 || d->heads % d->kv_heads != 0 || d->q_len < 0 || d->k_len < 0 || d->head_dim < 1) return false;
+    if (!(d->scale >= -3.402823466e+38f && d->scale <= 3.402823466e+38f)) return false;
+    if (((uintptr_t)d->q_lens & 3u) || ((uintptr_t)d->k_lens & 3u)) return false;
+    return !d->bias || valid_position_table(d->bias);
+}
+
+// sizes that the kernels' 32-bit counters hold
+bool covered(const egeria_attention_desc *d)
+{
+    return d->head_dim <= 128 && d->heads <= 65535 && d->q_len <= (1 << 29) && d->k_len <= (1 << 29);
+}
+
+// A tensor [batch, len, heads, dim]: 0 as it should be, else the error.  Elements of an output must not overlap: taken by rising
+// stride, every dimension's step has to clear what the ones below span.
+egeria_status check_view(const egeria_heads *t, const egeria_attention_desc *d, int len, int heads, bool output)
+{
+    if (!t) return EGERIA_ERR_INVALID_ARG;
+    if (t->batch_stride < 0 || t->token_stride < 0 || t->head_stride < 0) return EGERIA_ERR_INVALID_ARG;
+    if (d->batch == 0 || len == 0) return EGERIA_OK;
+    const size_t size = d->dtype == EGERIA_F32 ? 4 : 2;
+    if (!t->data || ((uintptr_t)t->data & (size - 1))) return EGERIA_ERR_INVALID_ARG;
+    int64_t n[3] = {d->batch, len, heads}, s[3] = {t->batch_stride, t->token_stride, t->head_stride};
+    for (int i = 0; i < 2; ++i)
+        for (int k = 0; k < 2 - i; ++k)
+            if (s[k] > s[k + 1]) {
+                const int64_t u = s[k], w = n[k];
+                s[k] = s[k + 1], n[k] = n[k + 1];
+                s[k + 1] = u, n[k + 1] = w;
+            }
+    unsigned __int128 span = (unsigned)d->head_dim;
+    for (int i = 0; i < 3; ++i) {
+        if (n[i] == 1) continue;
+        if (output && (unsigned __int128)s[i] < span) return EGERIA_ERR_INVALID_ARG;
+        span += (unsigned __int128)(n[i] - 1) * (unsigned __int128)s[i];
+    }
+    return span * size < ((unsigned __int128)1 << 62) ? EGERIA_OK : EGERIA_ERR_UNSUPPORTED;
+}
+
+View view_of(const egeria_heads *t) { return {(char *)t->data, t->batch_stride, t->token_stride, t->head_stride}; }
+
+AttnArgs make_args(const egeria_attention_desc *d)
+{
+    AttnArgs a = {};
+    a.q_lens = d->q_lens;
+    a.k_lens = d->k_lens;
+    a.batch = d->batch;
+    a.heads = d->heads;
+    a.kv_heads = d->kv_heads;
+    a.group = d->heads / d->kv_heads;
+    a.q_len = d->q_len;
+    a.k_len = d->k_len;
+    a.dim = d->head_dim;
+    a.causal = d->causal ? 1 : 0;
+    a.scale = d->scale;
+    if (d->bias) {
+        a.table = d->bias->table;
+        a.table_rows = d->bias->buckets;
+        a.b = make_buckets(d->bias);
+    }
+    return a;
+}
+
+int64_t row_tiles(const egeria_attention_desc *d) { return ((int64_t)d->q_len + kTileRows - 1) / kTileRows; }
+
+struct Plan {
+    size_t off_delta = 0, off_part = 0, total = 256;
+};
+Plan make_plan(const egeria_attention_desc *d, bool backward)
+{
+    Plan p;
+    if (!backward) return p;
+    size_t off = 0;
+    auto take = [&](size_t bytes) { size_t o = off; off += align_up(bytes, 256); return o; };
+    p.off_delta = take((size_t)d->batch * d->heads * d->q_len * 4);
+    p.off_part = take((size_t)d->batch * d->heads * row_tiles(d) * position_rows(d->bias) * 4);
+    p.total = off + 256;
+    return p;
+}
+
+}  // namespace
+
+}  // namespace egeria
+
+using namespace egeria;
+
+#define EG_TRY(expr)                                       \
+    do {                                                   \
+        const egeria_status s__ = (expr);                  \
+        if (s__ != EGERIA_OK) return s__;                  \
+    } while (0)
+#define EG_HIP(expr)                                   \
+    do {                                               \
+        if ((expr) != hipSuccess) return EGERIA_ERR_HIP; \
+    } while (0)
+
+extern "C" {
+
+size_t egeria_attention_workspace_bytes(const egeria_attention_desc *desc, int32_t backward)
+{
+    return valid_desc(desc) && covered(desc) ? make_plan(desc, backward != 0).total : 0;
+}
+
+egeria_status egeria_attention(const egeria_attention_desc *desc, const egeria_heads *q, const egeria_heads *k, const egeria_heads *v,
+                               const egeria_heads *out, float *lse, void *ws, size_t ws_bytes, void *stream)
+{
+    if (!valid_desc(desc)) return EGERIA_ERR_INVALID_ARG;
+    if (!covered(desc)) return EGERIA_ERR_UNSUPPORTED;
+    EG_TRY(check_view(q, desc, desc->q_len, desc->heads, false));
+    EG_TRY(check_view(k, desc, desc->k_len, desc->kv_heads, false));
+    EG_TRY(check_view(v, desc, desc->k_len, desc->kv_heads, false));
+    EG_TRY(check_view(out, desc, desc->q_len, desc->heads, true));
+    const int64_t rows = (int64_t)desc->batch * desc->heads * desc->q_len;
+    if ((rows > 0 && !lse) || ((uintptr_t)lse & 15u) || !ws || ((uintptr_t)ws & 15u)) return EGERIA_ERR_INVALID_ARG;
+    if (ws_bytes < make_plan(desc, false).total) return EGERIA_ERR_WORKSPACE_TOO_SMALL;
+    if (rows == 0) return EGERIA_OK;
+    if (rows / 4 + 1 > 0x7fffffffLL) return EGERIA_ERR_UNSUPPORTED;
+    AttnArgs a = make_args(desc);
+    a.q = view_of(q), a.k = view_of(k), a.v = view_of(v), a.o = view_of(out);
+    a.lse = lse;
+    const dim3 grid((unsigned)((rows + 3) / 4));
+    if (desc->dtype == EGERIA_F32) EG_HIP(launch_k(EGERIA_KERNEL_ATTENTION, attention_kernel<float>, grid, dim3(256), 0, (hipStream_t)stream, a));
+    else EG_HIP(launch_k(EGERIA_KERNEL_ATTENTION, attention_kernel<uint16_t>, grid, dim3(256), 0, (hipStream_t)stream, a));
+    return EGERIA_OK;
+}
+
+egeria_status egeria_attention_backward(const egeria_attention_desc *desc, const egeria_heads *dout, const egeria_heads *q,
+                                        const egeria_heads *k, const egeria_heads *v, const egeria_heads *out, const float *lse,
+                                        const egeria_heads *dq, const egeria_heads *dk, const egeria_heads *dv, float *dtable, void *ws,
+                                        size_t ws_bytes, void *stream)
+{
+    if (!valid_desc(desc)) return EGERIA_ERR_INVALID_ARG;
+    if (!covered(desc)) return EGERIA_ERR_UNSUPPORTED;
+    for (const egeria_heads *t : {dout, q, out}) EG_TRY(check_view(t, desc, desc->q_len, desc->heads, false));
+    for (const egeria_heads *t : {k, v}) EG_TRY(check_view(t, desc, desc->k_len, desc->kv_heads, false));
+    EG_TRY(check_view(dq, desc, desc->q_len, desc->heads, true));
+    for (const egeria_heads *t : {dk, dv}) EG_TRY(check_view(t, desc, desc->k_len, desc->kv_heads, true));
+    const int64_t rows = (int64_t)desc->batch * desc->heads * desc->q_len, keys = (int64_t)desc->batch * desc->kv_heads * desc->k_len;
+    if ((rows > 0 && !lse) || ((uintptr_t)lse & 15u) || !ws || ((uintptr_t)ws & 15u)) return EGERIA_ERR_INVALID_ARG;
+    if ((dtable && !desc->bias) || ((uintptr_t)dtable & 15u)) return EGERIA_ERR_INVALID_ARG;
+    const Plan p = make_plan(desc, true);
+    if (ws_bytes < p.total) return EGERIA_ERR_WORKSPACE_TOO_SMALL;
+    const int64_t tiles = (int64_t)desc->batch * desc->heads * row_tiles(desc);
+    if (tiles > 0x7fffffffLL || keys / 4 + 1 > 0x7fffffffLL) return EGERIA_ERR_UNSUPPORTED;
+    AttnArgs a = make_args(desc);
+    a.d_o = view_of(dout), a.q = view_of(q), a.k = view_of(k), a.v = view_of(v), a.o = view_of(out);
+    a.dq = view_of(dq), a.dk = view_of(dk), a.dv = view_of(dv);
+    a.lse = const_cast<float *>(lse);
+    a.delta = (float *)((char *)ws + p.off_delta);
+    a.partials = dtable ? (float *)((char *)ws + p.off_part) : nullptr;
+    hipStream_t st = (hipStream_t)stream;
+    const bool f32 = desc->dtype == EGERIA_F32;
+    auto go = [&](auto kernel, int64_t blocks) { return launch_k(EGERIA_KERNEL_ATTENTION, kernel, dim3((unsigned)blocks), dim3(256), 0, st, a); };
+    if (tiles > 0) EG_HIP(f32 ? go(attention_dq_kernel<float>, tiles) : go(attention_dq_kernel<uint16_t>, tiles));
+    if (keys > 0) EG_HIP(f32 ? go(attention_dkv_kernel<float>, (keys + 3) / 4) : go(attention_dkv_kernel<uint16_t>, (keys + 3) / 4));
+    if (dtable) EG_HIP(launch_table_reduce(a.partials, a.heads, (int64_t)a.batch * row_tiles(desc), a.table_rows, dtable, st));
+    return EGERIA_OK;
+}
+
+}  // extern "C"

@@ -1,0 +1,296 @@
+// The learned relative position bias as a tensor and the gradient of its table (definition in position.hpp).  Both are bound by
+// memory: one writes heads * q_len * k_len values, the other reads batch times as many.
+//
+//   bias[h, i, j] = table[bucket(j - i - offset), h]
+//   dtable[n, h]  = sum over b, i, j with bucket(j - i - offset) = n of dbias[b, h, i, j]
+#include "position.hpp"
+
+namespace egeria {
+
+namespace {
+
+constexpr int kRows = 8;            // rows of a thread's patch: kRows x 16 bytes, kRows + values - 1 distances
+
+// LDS word of entry i of a table that the 64 lanes of a wave read 8 entries apart: one word of padding every 64 keeps them on
+// different banks.
+__device__ __forceinline__ int spread(int i) { return i + (i >> 6); }
+
+template <typename T> struct Unit;
+template <> struct Unit<float> {
+    static constexpr int N = 4;
+    typedef float vec __attribute__((ext_vector_type(4), aligned(4)));
+};
+template <> struct Unit<uint16_t> {
+    static constexpr int N = 8;
+    typedef uint16_t vec __attribute__((ext_vector_type(8), aligned(2)));
+};
+__device__ __forceinline__ float widen(float v) { return v; }
+__device__ __forceinline__ float widen(uint16_t v) { return bf16_to_f32(v); }
+template <typename T> __device__ __forceinline__ T narrow(float v);
+template <> __device__ __forceinline__ float narrow<float>(float v) { return v; }
+template <> __device__ __forceinline__ uint16_t narrow<uint16_t>(float v)
+{
+    return __builtin_bit_cast(uint16_t, (__bf16)v);
+}
+
+// One workgroup: `rows` rows (a multiple of kRows) of one head, 256 units of 16 bytes of their columns.
+template <typename T>
+__global__ __launch_bounds__(256) void position_bias_kernel(Buckets b, const float *__restrict__ table, int heads, int q_len, int k_len,
+                                                            int offset, int rows, uint32_t row_blocks, uint32_t col_blocks,
+                                                            T *__restrict__ out)
+{
+    constexpr int N = Unit<T>::N;
+    typedef typename Unit<T>::vec vec;
+    extern __shared__ float lut[];
+    const uint32_t p = xcd_piece(blockIdx.x, gridDim.x);
+    const uint32_t cb = p % col_blocks, rb = p / col_blocks % row_blocks, h = p / col_blocks / row_blocks;
+    const int entries = b.both ? 2 * b.far + 1 : b.far + 1;
+    for (int i = threadIdx.x; i < entries; i += 256) lut[spread(i)] = table[bucket_of_entry(b, i) * heads + h];
+    __syncthreads();
+    const int j0 = (int)(cb * 256 + threadIdx.x) * N;
+    if (j0 >= k_len) return;
+    const int last = (int)rb * rows + rows < q_len ? (int)rb * rows + rows : q_len;
+    for (int i0 = rb * rows; i0 < last; i0 += kRows) {
+        T v[kRows + N - 1];                                        // distances first, first + 1, ...
+        const int first = j0 - (i0 + kRows - 1) - offset;
+#pragma unroll
+        for (int e = 0; e < kRows + N - 1; ++e) v[e] = narrow<T>(lut[spread(distance_index(b, first + e))]);
+#pragma unroll
+        for (int r = 0; r < kRows; ++r) {
+            if (i0 + r >= last) break;
+            T *dst = out + ((int64_t)h * q_len + i0 + r) * k_len + j0;
+            if (j0 + N <= k_len) {
+                vec w;
+#pragma unroll
+                for (int e = 0; e < N; ++e) w[e] = v[kRows - 1 - r + e];
+                *(vec *)dst = w;
+            } else {
+#pragma unroll
+                for (int e = 0; e < N; ++e)
+                    if (j0 + e < k_len) dst[e] = v[kRows - 1 - r + e];
+            }
+        }
+    }
+}
+
+// One workgroup: the same piece of the rows and columns, summed over its share of the batch.  A thread adds up its patch along the
+// diagonals in registers, over the batch, then the diagonals' sums go to a table by distance of its wave in LDS.  The lanes of a
+// wave add to different entries at each step and a wave's additions are in order: the result does not depend on timing.
+template <typename T>
+__global__ __launch_bounds__(256) void position_bias_backward_kernel(Buckets b, const T *__restrict__ dbias, int64_t batch, int heads,
+                                                                     int q_len, int k_len, int offset, int rows, uint32_t row_blocks,
+                                                                     uint32_t col_blocks, uint32_t shares, int rows_of_table,
+                                                                     float *__restrict__ partials)
+{
+    constexpr int N = Unit<T>::N;
+    typedef typename Unit<T>::vec vec;
+    extern __shared__ float sums[];                                // [4 waves][stride]
+    const uint32_t p = xcd_piece(blockIdx.x, gridDim.x);
+    const uint32_t cb = p % col_blocks, rb = p / col_blocks % row_blocks, sh = p / col_blocks / row_blocks % shares;
+    const uint32_t h = p / col_blocks / row_blocks / shares;
+    const int entries = b.both ? 2 * b.far + 1 : b.far + 1, stride = spread(entries - 1) + 1;
+    for (int i = threadIdx.x; i < 4 * stride; i += 256) sums[i] = 0.0f;
+    __syncthreads();
+    float *mine = sums + (threadIdx.x >> 6) * stride;
+    const int64_t b0 = batch * sh / shares, b1 = batch * (sh + 1) / shares;
+    const int j0 = (int)(cb * 256 + threadIdx.x) * N;
+    const int last = (int)rb * rows + rows < q_len ? (int)rb * rows + rows : q_len;
+    float left = 0.0f, right = 0.0f;                               // patches whose distances all lie beyond the table
+    const int hi = b.both ? b.far : 0;
+    for (int i0 = rb * rows; i0 < last; i0 += kRows) {
+        float d[kRows + N - 1];
+#pragma unroll
+        for (int e = 0; e < kRows + N - 1; ++e) d[e] = 0.0f;
+        if (j0 < k_len)
+            for (int64_t n = b0; n < b1; ++n) {
+                const T *src = dbias + ((n * heads + h) * q_len + i0) * k_len + j0;
+                vec w[kRows];
+#pragma unroll
+                for (int r = 0; r < kRows; ++r) {
+                    w[r] = vec(0);
+                    if (i0 + r < last) {
+                        if (j0 + N <= k_len) w[r] = *(const vec *)(src + (int64_t)r * k_len);
+                        else {
+#pragma unroll
+                            for (int e = 0; e < N; ++e)
+                                if (j0 + e < k_len) w[r][e] = src[(int64_t)r * k_len + e];
+                        }
+                    }
+                }
+#pragma unroll
+                for (int r = 0; r < kRows; ++r)
+#pragma unroll
+                    for (int e = 0; e < N; ++e) d[kRows - 1 - r + e] += widen((T)w[r][e]);
+            }
+        const int first = j0 - (i0 + kRows - 1) - offset;
+        if (first >= hi || first + kRows + N - 2 <= -b.far) {
+            float s = 0.0f;
+#pragma unroll
+            for (int e = 0; e < kRows + N - 1; ++e) s += d[e];
+            if (first >= hi) right += s;
+            else left += s;
+        } else {
+#pragma unroll
+            for (int e = 0; e < kRows + N - 1; ++e) {
+                const int rel = first + e;
+                // entries inside the table are different in every lane; what lies beyond its ends is the lane's own sum
+                if (rel <= -b.far) left += d[e];
+                else if (rel >= hi) right += d[e];
+                else __hip_atomic_fetch_add(&mine[spread(rel + b.far)], d[e], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
+            }
+        }
+    }
+    left = wave_sum(left);
+    right = wave_sum(right);
+    __syncthreads();
+    if ((threadIdx.x & 63) == 0) {
+        mine[0] += left;                                           // the ends of the table have the same buckets as what lies beyond
+        mine[spread(entries - 1)] += right;
+    }
+    __syncthreads();
+    // a bucket for each group of four lanes
+    const int64_t part = ((int64_t)sh * row_blocks + rb) * col_blocks + cb, parts = (int64_t)shares * row_blocks * col_blocks;
+    for (int n = threadIdx.x >> 2; n < rows_of_table; n += 64) {
+        int count;
+        const int at = entries_of_bucket(b, n, &count);
+        float s = 0.0f;
+        for (int i = threadIdx.x & 3; i < count; i += 4) {
+            const int w = spread(at + i);
+            s += (sums[w] + sums[w + stride]) + (sums[w + 2 * stride] + sums[w + 3 * stride]);
+        }
+        s += lane_xor<1>(s);
+        s += lane_xor<2>(s);
+        if ((threadIdx.x & 3) == 0) partials[((int64_t)h * parts + part) * rows_of_table + n] = s;
+    }
+}
+
+__global__ __launch_bounds__(256) void table_reduce_kernel(const float *__restrict__ partials, int heads, int64_t parts, int buckets,
+                                                           float *__restrict__ dtable)
+{
+    __shared__ double sm[256];
+    const int h = blockIdx.x;
+    // groups of `width` threads (a power of two, one for each bucket) take the parts in turn
+    int width = 1;
+    while (width < buckets) width <<= 1;
+    const int groups = 256 / width, g = threadIdx.x / width, n = threadIdx.x % width;
+    double s = 0.0;
+    if (n < buckets) {
+        const float *src = partials + (int64_t)h * parts * buckets + n;
+        int64_t i = g;
+        for (; i + 3 * groups < parts; i += 4 * groups) {
+            const float a = src[i * buckets], c = src[(i + groups) * buckets], d = src[(i + 2 * groups) * buckets], f = src[(i + 3 * groups) * buckets];
+            s += ((double)a + (double)c) + ((double)d + (double)f);
+        }
+        for (; i < parts; i += groups) s += (double)src[i * buckets];
+    }
+    sm[threadIdx.x] = s;
+    __syncthreads();
+    if (g == 0 && n < buckets) {
+        for (int k = 1; k < groups; ++k) s += sm[k * width + n];
+        dtable[n * heads + h] = (float)s;
+    }
+}
+
+// How the gradient's rows, columns and batch are dealt to workgroups: eight rows each where that is few workgroups, more where
+// that still leaves 2048, and the batch in shares where rows and columns alone do not give 1024.
+struct Pieces {
+    int rows;
+    uint32_t row_blocks, col_blocks, shares;
+};
+Pieces make_pieces(int64_t batch, int heads, int q_len, int k_len, int per_unit, bool split_batch)
+{
+    Pieces p;
+    p.col_blocks = (uint32_t)(((int64_t)k_len + 256 * per_unit - 1) / (256 * per_unit));
+    p.rows = kRows;
+    auto blocks = [&](int rows) { return (int64_t)((q_len + (int64_t)rows - 1) / rows) * p.col_blocks * heads; };
+    while (p.rows < 64 && blocks(2 * p.rows) >= 2048) p.rows *= 2;
+    p.row_blocks = (uint32_t)((q_len + (int64_t)p.rows - 1) / p.rows);
+    int64_t shares = 1;
+    if (split_batch) {
+        shares = blocks(p.rows) > 0 ? (1024 + blocks(p.rows) - 1) / blocks(p.rows) : 1;
+        shares = shares > batch ? batch : shares;
+        shares = shares < 1 ? 1 : shares;
+    }
+    p.shares = (uint32_t)shares;
+    return p;
+}
+
+bool valid_sizes(const egeria_position_table *t, int32_t heads, int32_t q_len, int32_t k_len, int32_t offset, egeria_dtype dt)
+{
+    if (!t || !valid_position_table(t) || heads < 1 || heads > 65535 || q_len < 0 || k_len < 0) return false;
+    if (dt != EGERIA_F32 && dt != EGERIA_BF16) return false;
+    return offset >= -(1 << 29) && offset <= (1 << 29) && q_len <= (1 << 29) && k_len <= (1 << 29);
+}
+
+int64_t parts_of(const Pieces &p) { return (int64_t)p.shares * p.row_blocks * p.col_blocks; }
+
+}  // namespace
+
+hipError_t launch_table_reduce(const float *partials, int heads, int64_t parts, int buckets, float *dtable, hipStream_t st)
+{
+    return launch_k(EGERIA_KERNEL_NONE, table_reduce_kernel, dim3((unsigned)heads), dim3(256), 0, st, partials, heads, parts, buckets, dtable);
+}
+
+}  // namespace egeria
+
+using namespace egeria;
+
+extern "C" {
+
+egeria_status egeria_position_bias(const egeria_position_table *t, int32_t heads, int32_t q_len, int32_t k_len, int32_t offset,
+                                   void *bias, egeria_dtype dt, void *stream)
+{
+    if (!valid_sizes(t, heads, q_len, k_len, offset, dt)) return EGERIA_ERR_INVALID_ARG;
+    if (q_len == 0 || k_len == 0) return EGERIA_OK;
+    if (!bias || ((uintptr_t)bias & 15u)) return EGERIA_ERR_INVALID_ARG;
+    const Buckets b = make_buckets(t);
+    const Pieces p = make_pieces(1, heads, q_len, k_len, dt == EGERIA_F32 ? 4 : 8, false);
+    const int64_t blocks = parts_of(p) * heads;
+    if (blocks > 0x7fffffffLL) return EGERIA_ERR_UNSUPPORTED;
+    const int entries = distance_entries(b);
+    const size_t lds = 4 * (size_t)(entries + entries / 64 + 1);
+    auto go = [&](auto kernel, auto *out) {
+        return launch_k(EGERIA_KERNEL_NONE, kernel, dim3((unsigned)blocks), dim3(256), lds, (hipStream_t)stream, b, t->table, (int)heads,
+                        (int)q_len, (int)k_len, (int)offset, p.rows, p.row_blocks, p.col_blocks, out);
+    };
+    const hipError_t e = dt == EGERIA_F32 ? go(position_bias_kernel<float>, (float *)bias) : go(position_bias_kernel<uint16_t>, (uint16_t *)bias);
+    return e == hipSuccess ? EGERIA_OK : EGERIA_ERR_HIP;
+}
+
+size_t egeria_position_bias_workspace_bytes(const egeria_position_table *t, int32_t batch, int32_t heads, int32_t q_len, int32_t k_len,
+                                            egeria_dtype dt)
+{
+    if (!valid_sizes(t, heads, q_len, k_len, 0, dt) || batch < 0) return 0;
+    const Pieces p = make_pieces(batch, heads, q_len, k_len, dt == EGERIA_F32 ? 4 : 8, true);
+    return align_up((size_t)parts_of(p) * heads * t->buckets * 4, 256) + 256;
+}
+
+egeria_status egeria_position_bias_backward(const egeria_position_table *t, const void *dbias, egeria_dtype dt, int32_t batch, int32_t heads,
+                                            int32_t q_len, int32_t k_len, int32_t offset, float *dtable, void *ws, size_t ws_bytes,
+                                            void *stream)
+{
+    if (!valid_sizes(t, heads, q_len, k_len, offset, dt) || batch < 0 || !dtable || ((uintptr_t)dtable & 15u)) return EGERIA_ERR_INVALID_ARG;
+    const bool none = batch == 0 || q_len == 0 || k_len == 0;
+    if (!none && (!dbias || ((uintptr_t)dbias & 15u))) return EGERIA_ERR_INVALID_ARG;
+    if (!ws || ((uintptr_t)ws & 15u)) return EGERIA_ERR_INVALID_ARG;
+    if (ws_bytes < egeria_position_bias_workspace_bytes(t, batch, heads, q_len, k_len, dt)) return EGERIA_ERR_WORKSPACE_TOO_SMALL;
+    hipStream_t st = (hipStream_t)stream;
+    float *partials = (float *)ws;
+    if (none) return launch_table_reduce(partials, heads, 0, t->buckets, dtable, st) == hipSuccess ? EGERIA_OK : EGERIA_ERR_HIP;
+    const Buckets b = make_buckets(t);
+    const Pieces p = make_pieces(batch, heads, q_len, k_len, dt == EGERIA_F32 ? 4 : 8, true);
+    const int64_t blocks = parts_of(p) * heads;
+    if (blocks > 0x7fffffffLL) return EGERIA_ERR_UNSUPPORTED;
+    const int entries = distance_entries(b);
+    const size_t lds = 16 * (size_t)(entries + entries / 64 + 1);
+    auto go = [&](auto kernel, auto *src) {
+        return launch_k(EGERIA_KERNEL_NONE, kernel, dim3((unsigned)blocks), dim3(256), lds, st, b, src, (int64_t)batch, (int)heads, (int)q_len,
+                        (int)k_len, (int)offset, p.rows, p.row_blocks, p.col_blocks, p.shares, (int)t->buckets, partials);
+    };
+    hipError_t e = dt == EGERIA_F32 ? go(position_bias_backward_kernel<float>, (const float *)dbias)
+                                    : go(position_bias_backward_kernel<uint16_t>, (const uint16_t *)dbias);
+    if (e == hipSuccess) e = launch_table_reduce(partials, heads, parts_of(p), t->buckets, dtable, st);
+    return e == hipSuccess ? EGERIA_OK : EGERIA_ERR_HIP;
+}
+
+}  // extern "C"

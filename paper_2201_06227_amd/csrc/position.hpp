@@ -1,0 +1,89 @@
+// The learned relative position bias: buckets of the distance between a key and a query, shared by the attention kernels and
+// by the kernels that make the bias and its gradient as tensors.
+//
+// A side has n buckets (half of them where both sides have their own).  With e = n / 2 and m = n - e, a distance below e has a
+// bucket to itself; bucket e + k holds the distances from e (M / e)^(k/m) on, up to the next border, and the last one all that
+// follow.  So a bucket is an interval of distances, and from the last border on (`far`, below the limit M) every distance has the
+// same one: a table of the distances -far ... far holds the whole function.
+#pragma once
+#include "common.hpp"
+#include <math.h>
+
+namespace egeria {
+
+constexpr int kMaxBuckets = 128;            // rows of a position table
+constexpr int kMaxDistance = 1024;          // largest max_distance: the tables by distance have to fit LDS
+
+struct Buckets {
+    int32_t n;                              // buckets of one side
+    int32_t e;                              // distances below e have buckets of their own
+    int32_t both;                           // the two sides have buckets of their own
+    int32_t far;                            // first distance of the last bucket
+    int32_t border[kMaxBuckets];            // first distance of bucket e + k
+};
+
+inline int position_rows(const egeria_position_table *t) { return t ? t->buckets : 0; }
+
+inline bool valid_position_table(const egeria_position_table *t)
+{
+    if (t->buckets < (t->bidirectional ? 4 : 2) || t->buckets > kMaxBuckets || (t->bidirectional && (t->buckets & 1))) return false;
+    const int n = t->bidirectional ? t->buckets / 2 : t->buckets;
+    return t->max_distance > n / 2 && t->max_distance <= kMaxDistance && t->table && !((uintptr_t)t->table & 15u);
+}
+
+// Borders in fp64; one that is within 1e-12 of a whole number is that number (they are whole where the power is, and pow() may
+// miss it by a rounding).
+inline Buckets make_buckets(const egeria_position_table *t)
+{
+    Buckets b;
+    b.both = t->bidirectional ? 1 : 0;
+    b.n = b.both ? t->buckets / 2 : t->buckets;
+    b.e = b.n / 2;
+    const int m = b.n - b.e;
+    for (int k = 0; k < kMaxBuckets; ++k) b.border[k] = 0x7fffffff;
+    for (int k = 0; k < m; ++k) {
+        const double x = (double)b.e * pow((double)t->max_distance / b.e, (double)k / m), near = rint(x);
+        b.border[k] = (int32_t)(fabs(x - near) <= 1e-12 * x ? near : ceil(x));
+    }
+    b.far = b.border[m - 1];
+    return b;
+}
+
+// Entries of the table by distance: index clamp(distance, -far, hi) + far with hi = far or, one-sided, 0.
+inline int distance_entries(const Buckets &b) { return b.both ? 2 * b.far + 1 : b.far + 1; }
+
+#ifdef __HIPCC__
+__device__ __forceinline__ int distance_index(const Buckets &b, int rel)
+{
+    const int hi = b.both ? b.far : 0;
+    return (rel < -b.far ? -b.far : (rel > hi ? hi : rel)) + b.far;
+}
+// bucket of entry `at` of the table by distance
+__device__ __forceinline__ int bucket_of_entry(const Buckets &b, int at)
+{
+    const int rel = at - b.far, dist = rel < 0 ? -rel : rel;
+    int k = dist;
+    if (dist >= b.e) {
+        k = b.e;
+        for (int i = 1; i < b.n - b.e; ++i) k += dist >= b.border[i] ? 1 : 0;
+    }
+    return rel > 0 ? b.n + k : k;           // (one-sided tables have no entry beyond 0)
+}
+// First entry of the table by distance that bucket `row` holds, and how many (0: none)
+__device__ __forceinline__ int entries_of_bucket(const Buckets &b, int row, int *count)
+{
+    const bool right = b.both && row >= b.n;
+    const int k = right ? row - b.n : row;
+    int lo = k < b.e ? k : b.border[k - b.e], hi;                   // distances lo ... hi - 1
+    if (k < b.e) hi = k + 1;
+    else hi = k == b.n - 1 ? b.far + 1 : b.border[k - b.e + 1];
+    if (right && lo == 0) lo = 1;                                   // distance 0 is the left side's
+    *count = hi > lo ? hi - lo : 0;
+    return right ? b.far + lo : b.far - hi + 1;
+}
+#endif
+
+// dtable [buckets, heads] of the partial sums [heads][parts][buckets], summed in this order in fp64
+hipError_t launch_table_reduce(const float *partials, int heads, int64_t parts, int buckets, float *dtable, hipStream_t st);
+
+}  // namespace egeria
