@@ -1,27 +1,9 @@
 // Attention of the training model's Transformer layers and its backward pass (include/egeria.h has the definition).
-#include "position.hpp"
+#include "attention.hpp"
 
 namespace egeria {
 
 namespace {
-
-struct View {
-    char *p;
-    int64_t sb, st, sh;                     // in elements
-};
-
-struct AttnArgs {
-    View q, k, v, o, d_o, dq, dk, dv;
-    float *lse;                             // [batch, heads, q_len]
-    float *delta;                           // [batch, heads, q_len], backward
-    float *partials;                        // [heads][batch * row tiles][buckets], backward with a table gradient
-    const int32_t *q_lens, *k_lens;
-    const float *table;                     // null: no bias
-    int32_t table_rows;
-    int32_t batch, heads, kv_heads, group, q_len, k_len, dim, causal;
-    float scale;
-    Buckets b;
-};
 
 template <typename T> __device__ __forceinline__ float load1(const View &v, int64_t off);
 template <> __device__ __forceinline__ float load1<float>(const View &v, int64_t off) { return ((const float *)v.p)[off]; }
@@ -31,12 +13,6 @@ template <> __device__ __forceinline__ void store1<float>(const View &v, int64_t
 template <> __device__ __forceinline__ void store1<uint16_t>(const View &v, int64_t off, float x)
 {
     ((uint16_t *)v.p)[off] = __builtin_bit_cast(uint16_t, (__bf16)x);
-}
-
-__device__ __forceinline__ int clamped(const int32_t *lens, int b, int most)
-{
-    const int n = lens ? lens[b] : most;
-    return n < 0 ? 0 : (n > most ? most : n);
 }
 
 // score of a pair that the lengths let see; minus infinity where it is hidden
@@ -55,39 +31,6 @@ __device__ __forceinline__ float score(const AttnArgs &a, int h, int64_t qo, int
 }
 
 constexpr int kTileRows = 64;
-
-// a wave per row
-template <typename T>
-__global__ __launch_bounds__(256) void attention_kernel(AttnArgs a)
-{
-    const int lane = threadIdx.x & 63;
-    const int64_t row = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
-    if (row >= (int64_t)a.batch * a.heads * a.q_len) return;
-    const int i = (int)(row % a.q_len), h = (int)(row / a.q_len % a.heads), b = (int)(row / a.q_len / a.heads);
-    const int nq = clamped(a.q_lens, b, a.q_len), nk = clamped(a.k_lens, b, a.k_len), shift = a.causal ? nk - nq : 0;
-    const int64_t qo = b * a.q.sb + i * a.q.st + h * a.q.sh;
-    float m = -INFINITY, l = 0.0f, o[2] = {0.0f, 0.0f};
-    for (int j0 = 0; i < nq && j0 < nk; j0 += 64) {
-        const int j = j0 + lane;
-        const float s = j < nk ? score<T>(a, h, qo, b * a.k.sb + j * a.k.st + h / a.group * a.k.sh, j - i - shift) : -INFINITY;
-        const float top = fmaxf(m, wave_max(s));
-        if (top == -INFINITY) continue;
-        const float keep = __builtin_amdgcn_exp2f((m - top) * 1.44269504f), p = __builtin_amdgcn_exp2f((s - top) * 1.44269504f);
-        l = l * keep + wave_sum(p);
-        m = top;
-        for (int c = 0; c < 2; ++c) o[c] *= keep;
-        for (int e = 0; e < 64 && j0 + e < nk; ++e) {
-            const float w = __shfl(p, e);
-            if (w == 0.0f) continue;
-            const int64_t vo = b * a.v.sb + (j0 + e) * a.v.st + h / a.group * a.v.sh;
-            for (int c = 0; c < 2; ++c)
-                if (lane + 64 * c < a.dim) o[c] = fmaf(w, load1<T>(a.v, vo + lane + 64 * c), o[c]);
-        }
-    }
-    for (int c = 0; c < 2; ++c)
-        if (lane + 64 * c < a.dim) store1<T>(a.o, b * a.o.sb + i * a.o.st + h * a.o.sh + lane + 64 * c, l > 0.0f ? o[c] / l : 0.0f);
-    if (lane == 0) a.lse[row] = l > 0.0f ? m + logf(l) : -INFINITY;
-}
 
 // p and ds of a pair
 template <typename T>
@@ -201,10 +144,12 @@ bool valid_desc(const egeria_attention_desc *d)
     return !d->bias || valid_position_table(d->bias);
 }
 
-// sizes that the kernels' 32-bit counters hold
+// sizes that the kernels' 32-bit counters and the workspace's 64-bit ones hold
 bool covered(const egeria_attention_desc *d)
 {
-    return d->head_dim <= 128 && d->heads <= 65535 && d->q_len <= (1 << 29) && d->k_len <= (1 << 29);
+    if (d->head_dim > 128 || d->heads > 65535 || d->q_len > (1 << 29) || d->k_len > (1 << 29)) return false;
+    const int64_t pairs = (int64_t)d->batch * d->heads;
+    return pairs < (1LL << 31) && pairs * d->q_len < (1LL << 38) && pairs * d->k_len < (1LL << 38);
 }
 
 // A tensor [batch, len, heads, dim]: 0 as it should be, else the error.  Elements of an output must not overlap: taken by rising
@@ -259,18 +204,55 @@ AttnArgs make_args(const egeria_attention_desc *d)
 
 int64_t row_tiles(const egeria_attention_desc *d) { return ((int64_t)d->q_len + kTileRows - 1) / kTileRows; }
 
+// Whether every row of a tensor starts on 16 bytes, holds whole units of 16 and 64 rows span less than 2 GiB.
+bool wide_rows(const egeria_heads *t, const egeria_attention_desc *d)
+{
+    const int64_t size = d->dtype == EGERIA_F32 ? 4 : 2;
+    return !((uintptr_t)t->data & 15u) && t->batch_stride * size % 16 == 0 && t->token_stride * size % 16 == 0 && t->head_stride * size % 16 == 0 &&
+           d->head_dim * size % 16 == 0 && t->token_stride * size < (0x7fffffffLL - 1024) / kRowTile;
+}
+
+int64_t few_tiles(const egeria_attention_desc *d)
+{
+    const int64_t rows = (int64_t)(d->heads / d->kv_heads) * d->q_len;
+    return (rows + kFewRows - 1) / kFewRows * d->batch * d->kv_heads;
+}
+
+// The forward kernel for few rows, and how many workgroups share a row tile's keys there (0: the other kernel).  A tile of 128 queries
+// leaves most of its waves without rows up to 32 queries; and where the tiles are few and the keys many, the keys have to be shared
+// to occupy the device.  Splits: up to two workgroups for each compute unit, of at least 256 keys.
+int few_splits(const egeria_attention_desc *d)
+{
+    const int64_t blocks = (int64_t)d->batch * d->heads * (((int64_t)d->q_len + kRowTile - 1) / kRowTile);
+    const int64_t tiles = few_tiles(d);
+    if (d->q_len > 32 && !(blocks < 64 && d->k_len >= 1024)) return 0;
+    if (tiles == 0) return 0;
+    int64_t n = (512 + tiles - 1) / tiles;
+    const int64_t most = ((int64_t)d->k_len + 255) / 256;
+    n = n > most ? most : n;
+    return n < 1 ? 1 : (int)n;
+}
+
 struct Plan {
-    size_t off_delta = 0, off_part = 0, total = 256;
+    size_t off_delta = 0, off_part = 0, off_o = 0, off_ml = 0, total = 0;
+    int splits = 0;
 };
 Plan make_plan(const egeria_attention_desc *d, bool backward)
 {
     Plan p;
-    if (!backward) return p;
-    size_t off = 0;
-    auto take = [&](size_t bytes) { size_t o = off; off += align_up(bytes, 256); return o; };
-    p.off_delta = take((size_t)d->batch * d->heads * d->q_len * 4);
-    p.off_part = take((size_t)d->batch * d->heads * row_tiles(d) * position_rows(d->bias) * 4);
-    p.total = off + 256;
+    auto take = [&](size_t bytes) { size_t o = p.total; p.total += align_up(bytes, 256); return o; };
+    take(256);
+    if (backward) {
+        p.off_delta = take((size_t)d->batch * d->heads * d->q_len * 4);
+        p.off_part = take((size_t)d->batch * d->heads * row_tiles(d) * position_rows(d->bias) * 4);
+        return p;
+    }
+    p.splits = few_splits(d);
+    if (p.splits > 1) {
+        const size_t rows = (size_t)few_tiles(d) * kFewRows * p.splits;
+        p.off_o = take(rows * (d->head_dim <= 64 ? 64 : 128) * 4);
+        p.off_ml = take(rows * 8);
+    }
     return p;
 }
 
@@ -308,15 +290,18 @@ egeria_status egeria_attention(const egeria_attention_desc *desc, const egeria_h
     EG_TRY(check_view(out, desc, desc->q_len, desc->heads, true));
     const int64_t rows = (int64_t)desc->batch * desc->heads * desc->q_len;
     if ((rows > 0 && !lse) || ((uintptr_t)lse & 15u) || !ws || ((uintptr_t)ws & 15u)) return EGERIA_ERR_INVALID_ARG;
-    if (ws_bytes < make_plan(desc, false).total) return EGERIA_ERR_WORKSPACE_TOO_SMALL;
+    const Plan p = make_plan(desc, false);
+    if (ws_bytes < p.total) return EGERIA_ERR_WORKSPACE_TOO_SMALL;
     if (rows == 0) return EGERIA_OK;
-    if (rows / 4 + 1 > 0x7fffffffLL) return EGERIA_ERR_UNSUPPORTED;
+    if ((p.splits ? few_tiles(desc) : rows / kRowTile + (int64_t)desc->batch * desc->heads) > (1 << 28)) return EGERIA_ERR_UNSUPPORTED;
     AttnArgs a = make_args(desc);
     a.q = view_of(q), a.k = view_of(k), a.v = view_of(v), a.o = view_of(out);
     a.lse = lse;
-    const dim3 grid((unsigned)((rows + 3) / 4));
-    if (desc->dtype == EGERIA_F32) EG_HIP(launch_k(EGERIA_KERNEL_ATTENTION, attention_kernel<float>, grid, dim3(256), 0, (hipStream_t)stream, a));
-    else EG_HIP(launch_k(EGERIA_KERNEL_ATTENTION, attention_kernel<uint16_t>, grid, dim3(256), 0, (hipStream_t)stream, a));
+    a.splits = p.splits;
+    a.split_o = (float *)((char *)ws + p.off_o);
+    a.split_ml = (float *)((char *)ws + p.off_ml);
+    const bool vec = wide_rows(q, desc) && wide_rows(k, desc) && wide_rows(v, desc) && wide_rows(out, desc);
+    EG_HIP((p.splits ? launch_attention_few : launch_attention_forward)(a, (egeria_dtype)desc->dtype, vec, (hipStream_t)stream));
     return EGERIA_OK;
 }
 

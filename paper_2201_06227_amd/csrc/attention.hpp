@@ -1,0 +1,283 @@
+// What the attention kernels share: arguments, operand tiles in LDS, matrix-core fragments.
+#pragma once
+#include "position.hpp"
+
+namespace egeria {
+
+struct View {
+    char *p;
+    int64_t sb, st, sh;                     // strides in elements
+};
+
+struct AttnArgs {
+    View q, k, v, o, d_o, dq, dk, dv;
+    float *lse;                             // [batch, heads, q_len]
+    float *delta;                           // [batch, heads, q_len], backward
+    float *partials;                        // [heads][batch * row tiles][buckets], backward with a table gradient
+    float *split_o, *split_ml;              // forward split over keys: partial outputs and row statistics
+    const int32_t *q_lens, *k_lens;
+    const float *table;                     // null: no bias
+    int32_t table_rows;
+    int32_t batch, heads, kv_heads, group, q_len, k_len, dim, causal;
+    int32_t splits;
+    float scale;
+    Buckets b;
+};
+
+constexpr int kRowTile = 128;               // queries (or keys, in the dk / dv kernel) of a workgroup
+constexpr int kKeyTile = 64;                // keys (queries) of one step
+constexpr int kFewRows = 32;                // rows of a workgroup of the kernel for few rows
+constexpr int kFewKeys = 32;                // keys that a wave of it takes at a time
+
+hipError_t launch_attention_forward(const AttnArgs &a, egeria_dtype dt, bool vec, hipStream_t st);
+// few rows: a.splits workgroups share a row tile's keys; more than one leaves partial results (split_o, split_ml) that a second
+// launch joins
+hipError_t launch_attention_few(const AttnArgs &a, egeria_dtype dt, bool vec, hipStream_t st);
+
+#ifdef __HIPCC__
+
+constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.69314718055994530942f;
+constexpr float kHidden = -1e30f;           // table entries up to this hide their pairs
+
+typedef __bf16 v8bf __attribute__((ext_vector_type(8)));
+typedef short v4s __attribute__((ext_vector_type(4)));
+typedef float v16f __attribute__((ext_vector_type(16)));
+typedef __attribute__((address_space(3))) v4s lds_v4s;
+typedef __attribute__((address_space(3))) v4u lds_v4u;
+typedef __attribute__((address_space(3))) float lds_f32;
+
+struct v8f {
+    float v[8];
+};
+
+__device__ __forceinline__ int clamped(const int32_t *lens, int b, int most)
+{
+    const int n = lens ? lens[b] : most;
+    return n < 0 ? 0 : (n > most ? most : n);
+}
+
+// Operand fragments of a 32 x 32 x 16 product: lane l holds row (A) or column (B) l % 32, eight consecutive values of the reduced
+// dimension from 8 (l / 32) on.  bf16: one instruction.  fp32: eight of depth two, which take element e of both halves: the same
+// sixteen products, so one layout serves both types.
+template <typename T> struct FragOf;
+template <> struct FragOf<uint16_t> { typedef v8bf type; };
+template <> struct FragOf<float> { typedef v8f type; };
+
+__device__ __forceinline__ v16f mma(v8bf a, v8bf b, v16f c) { return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0); }
+__device__ __forceinline__ v16f mma(const v8f &a, const v8f &b, v16f c)
+{
+#pragma unroll
+    for (int e = 0; e < 8; ++e) c = __builtin_amdgcn_mfma_f32_32x32x2f32(a.v[e], b.v[e], c, 0, 0, 0);
+    return c;
+}
+
+// A 32 x 32 result holds, in register r of lane l, row 8 (r / 4) + 4 (l / 32) + r % 4 of column l % 32.  Registers 8 s ... 8 s + 7 are
+// therefore, for the lane's column, the rows 16 s + {4 half + 0..3, 8 + 4 half + 0..3}: an operand of the next product over those 16
+// rows, if the other operand is read in the same order (col_frag).  So probabilities go from one product to the next in
+// registers.
+template <typename T> __device__ __forceinline__ typename FragOf<T>::type pack(const v16f &c, int s);
+template <> __device__ __forceinline__ v8bf pack<uint16_t>(const v16f &c, int s)
+{
+    v8bf f;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) f[e] = (__bf16)c[8 * s + e];
+    return f;
+}
+template <> __device__ __forceinline__ v8f pack<float>(const v16f &c, int s)
+{
+    v8f f;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) f.v[e] = c[8 * s + e];
+    return f;
+}
+__device__ __forceinline__ int row_of(int r, int half) { return 8 * (r >> 2) + 4 * half + (r & 3); }
+
+// Tiles of rows of D values in LDS, read along rows (row_frag: 16 bytes of 32 rows) and across them (col_frag: 4 rows of 32 columns,
+// transposed by the read itself for bf16).  A row is kept in units of 16 bytes, unit u of row r at slot u ^ turn(r).  The 64 banks
+// of 4 bytes hold 256 bytes, i.e. 16 units: the 16 rows that a quarter of a wave reads a unit of have 16 different (row, slot) places
+// if turn() takes different values over the rows that share a place; and of the four rows that half a wave reads 4 units of each
+// across, those that share places have turn() differ in the bits above the lowest two.  Rows of 128 bytes (two to a line of banks): the
+// bits of r / 2 in reverse; longer rows: r with its lowest two bits on top.
+template <typename T, int D>
+struct Tile {
+    static constexpr int kUnits = D * (int)sizeof(T) / 16, kRowBytes = D * (int)sizeof(T);
+    static __device__ __forceinline__ int turn(int r)
+    {
+        if constexpr (kUnits == 8) return ((r >> 1) & 1) << 2 | ((r >> 2) & 1) << 1 | ((r >> 3) & 1);
+        else return (r & 3) << 2 | ((r >> 2) & 3);
+    }
+    static __device__ __forceinline__ uint32_t at(int r, int u) { return (uint32_t)(r * kRowBytes + ((u ^ turn(r)) << 4)); }
+
+    typedef typename FragOf<T>::type frag;
+
+    // rows r0 ... r0 + 31, values 16 kk ... 16 kk + 15
+    static __device__ __forceinline__ frag row_frag(uint32_t lds, int r0, int kk, int lane)
+    {
+        const int r = r0 + (lane & 31), half = lane >> 5;
+        if constexpr (sizeof(T) == 2) {
+            return __builtin_bit_cast(v8bf, *(const lds_v4u *)(uintptr_t)(lds + at(r, 2 * kk + half)));
+        } else {
+            const v4u lo = *(const lds_v4u *)(uintptr_t)(lds + at(r, 4 * kk + 2 * half)), hi = *(const lds_v4u *)(uintptr_t)(lds + at(r, 4 * kk + 2 * half + 1));
+            v8f f;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                f.v[e] = __uint_as_float(lo[e]);
+                f.v[4 + e] = __uint_as_float(hi[e]);
+            }
+            return f;
+        }
+    }
+    // columns 32 db ... 32 db + 31 of the 16 rows from r0 on, in the order of pack()
+    static __device__ __forceinline__ frag col_frag(uint32_t lds, int r0, int db, int lane)
+    {
+        const int half = lane >> 5;
+        if constexpr (sizeof(T) == 2) {
+            // in each group of 16 lanes, lane i addresses 4 columns of row i / 4 and receives column i of the four rows
+            const int r = r0 + 4 * half + ((lane & 15) >> 2), u = 4 * db + ((lane >> 4) & 1) * 2 + ((lane & 3) >> 1);
+            const v4s lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4s *)(uintptr_t)(lds + at(r, u) + (lane & 1) * 8));
+            const v4s hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4s *)(uintptr_t)(lds + at(r + 8, u) + (lane & 1) * 8));
+            return __builtin_bit_cast(v8bf, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+        } else {
+            const int c = 32 * db + (lane & 31);
+            v8f f;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                const int r = r0 + 4 * half + (e & 3) + 8 * (e >> 2);
+                f.v[e] = *(const lds_f32 *)(uintptr_t)(lds + at(r, c >> 2) + (c & 3) * 4);
+            }
+            return f;
+        }
+    }
+};
+
+// Reads rows of one head of a tensor [.., token, .., feature].
+// VEC: rows start on 16 bytes, hold a whole number of 16-byte units, and 64 of them span less than 2 GiB: buffer loads, straight into
+// LDS.  A unit beyond the row's end or of a token at or beyond `tokens` is asked for beyond the buffer and arrives as zeros.
+// Otherwise: element by element.
+template <typename T, int D, bool VEC>
+struct Rows {
+    const char *base;
+    int64_t row_bytes;
+    int tokens, dim;
+
+    __device__ __forceinline__ void open(const View &v, int b, int h, int n, int d)
+    {
+        base = v.p + ((int64_t)b * v.sb + (int64_t)h * v.sh) * (int64_t)sizeof(T);
+        row_bytes = v.st * (int64_t)sizeof(T);
+        tokens = n;
+        dim = d;
+    }
+    // 16 bytes: unit u of token t
+    __device__ __forceinline__ v4u unit(int t, int u) const
+    {
+        constexpr int N = 16 / (int)sizeof(T);
+        union { v4u w; T e[N]; } x;
+        x.w = v4u(0);
+        if (t < tokens && u * N < dim) {
+            const char *p = base + (int64_t)t * row_bytes + u * 16;
+            if constexpr (VEC) x.w = *(const v4u *)p;
+            else {
+#pragma unroll
+                for (int e = 0; e < N; ++e)
+                    if (u * N + e < dim) x.e[e] = ((const T *)p)[e];
+            }
+        }
+        return x.w;
+    }
+    // fragment of the 32 tokens from t0 on, values 16 kk ...
+    __device__ __forceinline__ typename FragOf<T>::type frag(int t0, int kk, int lane) const
+    {
+        const int t = t0 + (lane & 31), half = lane >> 5;
+        if constexpr (sizeof(T) == 2) return __builtin_bit_cast(v8bf, unit(t, 2 * kk + half));
+        else {
+            const v4u lo = unit(t, 4 * kk + 2 * half), hi = unit(t, 4 * kk + 2 * half + 1);
+            v8f f;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                f.v[e] = __uint_as_float(lo[e]);
+                f.v[4 + e] = __uint_as_float(hi[e]);
+            }
+            return f;
+        }
+    }
+    // N tokens from t0 on into a tile, by the THREADS threads numbered tid (whole waves); the requests of the VEC form are
+    // outstanding until an explicit wait
+    template <int N, int THREADS>
+    __device__ __forceinline__ void stage(uint32_t lds, int t0, int tid) const
+    {
+        typedef Tile<T, D> tile;
+        constexpr int kUnits = tile::kUnits, kSteps = N * kUnits / THREADS;
+        static_assert(N * kUnits % THREADS == 0, "whole requests");
+        if constexpr (VEC) {
+            const uint64_t at = (uint64_t)(base + (int64_t)t0 * row_bytes);
+            v4i rsrc;
+            rsrc[0] = __builtin_amdgcn_readfirstlane((int)(uint32_t)at);
+            rsrc[1] = __builtin_amdgcn_readfirstlane((int)(uint32_t)(at >> 32) & 0xffff);
+            rsrc[2] = 0x7fffffff;
+            rsrc[3] = kBufferWord;
+            const uint32_t first = lds + (uint32_t)__builtin_amdgcn_readfirstlane(tid & ~63) * 16u;
+            const uint32_t step = (uint32_t)row_bytes;
+            const int dim_units = dim * (int)sizeof(T) / 16;
+#pragma unroll
+            for (int i = 0; i < kSteps; ++i) {
+                const int n = i * THREADS + tid, r = n / kUnits, u = (n % kUnits) ^ tile::turn(r);
+                const uint32_t off = t0 + r < tokens && u < dim_units ? (uint32_t)r * step + (uint32_t)u * 16u : 0x80000000u;
+                load_to_lds_b128(rsrc, first + (uint32_t)(i * THREADS * 16), off);
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < kSteps; ++i) {
+                const int n = i * THREADS + tid, r = n / kUnits, u = n % kUnits;
+                *(lds_v4u *)(uintptr_t)(lds + tile::at(r, u)) = unit(t0 + r, u);
+            }
+        }
+    }
+};
+
+// Writes four values: features f ... f + 3 of a token
+template <typename T, bool VEC>
+__device__ __forceinline__ void store4(T *row, int f, int dim, float x0, float x1, float x2, float x3)
+{
+    if constexpr (sizeof(T) == 2) {
+        union { v2u w; __bf16 e[4]; } x;
+        x.e[0] = (__bf16)x0, x.e[1] = (__bf16)x1, x.e[2] = (__bf16)x2, x.e[3] = (__bf16)x3;
+        if constexpr (VEC) {
+            if (f < dim) *(v2u *)(row + f) = x.w;
+        } else {
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                if (f + e < dim) ((__bf16 *)row)[f + e] = x.e[e];
+        }
+    } else {
+        const float x[4] = {x0, x1, x2, x3};
+        if constexpr (VEC) {
+            if (f < dim) *(float4 *)(row + f) = make_float4(x0, x1, x2, x3);
+        } else {
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                if (f + e < dim) row[f + e] = x[e];
+        }
+    }
+}
+
+// The table by distance of one head in LDS, in units of the scores' base-2 exponent; hidden entries are minus infinity.
+__device__ __forceinline__ float table_value(const float *table, int row, int heads, int h)
+{
+    const float t = table[row * heads + h];
+    return t <= kHidden ? -INFINITY : t * kLog2e;
+}
+
+template <typename K>
+inline hipError_t allow_lds(K kernel, size_t bytes, bool (&done)[kMaxDevices])
+{
+    const int dev = current_device();
+    if (dev < 0) return hipErrorInvalidDevice;
+    if (done[dev] || bytes <= 65536) return hipSuccess;
+    const hipError_t e = hipFuncSetAttribute((const void *)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, 156 * 1024);
+    if (e == hipSuccess) done[dev] = true;
+    return e;
+}
+
+#endif
+
+}  // namespace egeria
