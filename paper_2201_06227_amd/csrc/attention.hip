@@ -5,136 +5,6 @@ namespace egeria {
 
 namespace {
 
-template <typename T> __device__ __forceinline__ float load1(const View &v, int64_t off);
-template <> __device__ __forceinline__ float load1<float>(const View &v, int64_t off) { return ((const float *)v.p)[off]; }
-template <> __device__ __forceinline__ float load1<uint16_t>(const View &v, int64_t off) { return bf16_to_f32(((const uint16_t *)v.p)[off]); }
-template <typename T> __device__ __forceinline__ void store1(const View &v, int64_t off, float x);
-template <> __device__ __forceinline__ void store1<float>(const View &v, int64_t off, float x) { ((float *)v.p)[off] = x; }
-template <> __device__ __forceinline__ void store1<uint16_t>(const View &v, int64_t off, float x)
-{
-    ((uint16_t *)v.p)[off] = __builtin_bit_cast(uint16_t, (__bf16)x);
-}
-
-// score of a pair that the lengths let see; minus infinity where it is hidden
-template <typename T>
-__device__ __forceinline__ float score(const AttnArgs &a, int h, int64_t qo, int64_t ko, int rel)
-{
-    if (a.causal && rel > 0) return -INFINITY;
-    float s = 0.0f;
-    for (int d = 0; d < a.dim; ++d) s = fmaf(load1<T>(a.q, qo + d), load1<T>(a.k, ko + d), s);
-    s *= a.scale;
-    if (a.table) {
-        const float t = a.table[bucket_of_entry(a.b, distance_index(a.b, rel)) * a.heads + h];
-        s = t <= -1e30f ? -INFINITY : s + t;
-    }
-    return s;
-}
-
-constexpr int kTileRows = 64;
-
-// p and ds of a pair
-template <typename T>
-__device__ __forceinline__ float pair_grad(const AttnArgs &a, int h, int64_t qo, int64_t oo, int64_t ko, int64_t vo, int rel, float lse, float delta, float *p)
-{
-    const float s = score<T>(a, h, qo, ko, rel);
-    *p = s == -INFINITY || lse == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f((s - lse) * 1.44269504f);
-    float dp = 0.0f;
-    for (int d = 0; d < a.dim; ++d) dp = fmaf(load1<T>(a.d_o, oo + d), load1<T>(a.v, vo + d), dp);
-    return *p == 0.0f ? 0.0f : *p * (dp - delta);
-}
-
-// dq, delta and the partial sums of the table's gradient: kTileRows queries per workgroup, a wave per row
-template <typename T>
-__global__ __launch_bounds__(256) void attention_dq_kernel(AttnArgs a)
-{
-    __shared__ float sums[4][kMaxBuckets];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const int tiles = (a.q_len + kTileRows - 1) / kTileRows, tile = blockIdx.x % tiles;
-    const int h = blockIdx.x / tiles % a.heads, b = blockIdx.x / tiles / a.heads;
-    const int nq = clamped(a.q_lens, b, a.q_len), nk = clamped(a.k_lens, b, a.k_len), shift = a.causal ? nk - nq : 0;
-    float acc[2] = {0.0f, 0.0f};
-    for (int i = tile * kTileRows + wave; i < (tile + 1) * kTileRows && i < a.q_len; i += 4) {
-        const int64_t qo = b * a.q.sb + i * a.q.st + h * a.q.sh, oo = b * a.d_o.sb + i * a.d_o.st + h * a.d_o.sh;
-        const int64_t uo = b * a.o.sb + i * a.o.st + h * a.o.sh, row = ((int64_t)b * a.heads + h) * a.q_len + i;
-        float o[2] = {0.0f, 0.0f}, delta = 0.0f;
-        if (i < nq) {
-            for (int d = lane; d < a.dim; d += 64) delta = fmaf(load1<T>(a.d_o, oo + d), load1<T>(a.o, uo + d), delta);
-            delta = wave_sum(delta);
-            const float lse = a.lse[row];
-            for (int j0 = 0; j0 < nk; j0 += 64) {
-                const int j = j0 + lane, rel = j - i - shift;
-                float p = 0.0f, ds = 0.0f;
-                if (j < nk)
-                    ds = pair_grad<T>(a, h, qo, oo, b * a.k.sb + j * a.k.st + h / a.group * a.k.sh,
-                                      b * a.v.sb + j * a.v.st + h / a.group * a.v.sh, rel, lse, delta, &p);
-                const int bucket = a.table ? bucket_of_entry(a.b, distance_index(a.b, rel)) : 0;
-                for (int e = 0; e < 64 && j0 + e < nk; ++e) {
-                    const float w = __shfl(ds, e);
-                    if (a.partials) {
-                        const int n = __shfl(bucket, e);
-                        if (lane == (n & 63)) acc[n >> 6] += w;
-                    }
-                    if (w == 0.0f) continue;
-                    const int64_t ko = b * a.k.sb + (j0 + e) * a.k.st + h / a.group * a.k.sh;
-                    for (int c = 0; c < 2; ++c)
-                        if (lane + 64 * c < a.dim) o[c] = fmaf(w, load1<T>(a.k, ko + lane + 64 * c), o[c]);
-                }
-            }
-        }
-        if (lane == 0) a.delta[row] = delta;
-        for (int c = 0; c < 2; ++c)
-            if (lane + 64 * c < a.dim) store1<T>(a.dq, b * a.dq.sb + i * a.dq.st + h * a.dq.sh + lane + 64 * c, o[c] * a.scale);
-    }
-    if (a.partials) {
-        sums[wave][lane] = acc[0];
-        sums[wave][lane + 64] = acc[1];
-        __syncthreads();
-        for (int n = threadIdx.x; n < a.table_rows; n += 256)
-            a.partials[((int64_t)h * a.batch * tiles + (int64_t)b * tiles + tile) * a.table_rows + n] =
-                (sums[0][n] + sums[1][n]) + (sums[2][n] + sums[3][n]);
-    }
-}
-
-// dk and dv: a wave per key
-template <typename T>
-__global__ __launch_bounds__(256) void attention_dkv_kernel(AttnArgs a)
-{
-    const int lane = threadIdx.x & 63;
-    const int64_t row = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
-    if (row >= (int64_t)a.batch * a.kv_heads * a.k_len) return;
-    const int j = (int)(row % a.k_len), g = (int)(row / a.k_len % a.kv_heads), b = (int)(row / a.k_len / a.kv_heads);
-    const int nq = clamped(a.q_lens, b, a.q_len), nk = clamped(a.k_lens, b, a.k_len), shift = a.causal ? nk - nq : 0;
-    float dk[2] = {0.0f, 0.0f}, dv[2] = {0.0f, 0.0f};
-    const int64_t ko = b * a.k.sb + j * a.k.st + g * a.k.sh, vo = b * a.v.sb + j * a.v.st + g * a.v.sh;
-    for (int h = g * a.group; j < nk && h < (g + 1) * a.group; ++h)
-        for (int i0 = 0; i0 < nq; i0 += 64) {
-            const int i = i0 + lane;
-            float p = 0.0f, ds = 0.0f;
-            if (i < nq) {
-                const int64_t at = ((int64_t)b * a.heads + h) * a.q_len + i;
-                ds = pair_grad<T>(a, h, b * a.q.sb + i * a.q.st + h * a.q.sh, b * a.d_o.sb + i * a.d_o.st + h * a.d_o.sh, ko, vo,
-                                  j - i - shift, a.lse[at], a.delta[at], &p);
-            }
-            for (int e = 0; e < 64 && i0 + e < nq; ++e) {
-                const float w = __shfl(ds, e), u = __shfl(p, e);
-                if (u == 0.0f) continue;
-                const int64_t qo = b * a.q.sb + (i0 + e) * a.q.st + h * a.q.sh, oo = b * a.d_o.sb + (i0 + e) * a.d_o.st + h * a.d_o.sh;
-                for (int c = 0; c < 2; ++c)
-                    if (lane + 64 * c < a.dim) {
-                        dk[c] = fmaf(w, load1<T>(a.q, qo + lane + 64 * c), dk[c]);
-                        dv[c] = fmaf(u, load1<T>(a.d_o, oo + lane + 64 * c), dv[c]);
-                    }
-            }
-        }
-    for (int c = 0; c < 2; ++c)
-        if (lane + 64 * c < a.dim) {
-            store1<T>(a.dk, b * a.dk.sb + j * a.dk.st + g * a.dk.sh + lane + 64 * c, dk[c] * a.scale);
-            store1<T>(a.dv, b * a.dv.sb + j * a.dv.st + g * a.dv.sh + lane + 64 * c, dv[c]);
-        }
-}
-
-// ---- host side -------------------------------------------------------------------------------------------------
-
 bool valid_desc(const egeria_attention_desc *d)
 {
     if (!d || (d->dtype != EGERIA_F32 && d->dtype != EGERIA_BF16)) return false;
@@ -202,7 +72,7 @@ AttnArgs make_args(const egeria_attention_desc *d)
     return a;
 }
 
-int64_t row_tiles(const egeria_attention_desc *d) { return ((int64_t)d->q_len + kTileRows - 1) / kTileRows; }
+int64_t row_tiles(const egeria_attention_desc *d) { return ((int64_t)d->q_len + kRowTile - 1) / kRowTile; }
 
 // Whether every row of a tensor starts on 16 bytes, holds whole units of 16 and 64 rows span less than 2 GiB.
 bool wide_rows(const egeria_heads *t, const egeria_attention_desc *d)
@@ -321,8 +191,7 @@ egeria_status egeria_attention_backward(const egeria_attention_desc *desc, const
     if ((dtable && !desc->bias) || ((uintptr_t)dtable & 15u)) return EGERIA_ERR_INVALID_ARG;
     const Plan p = make_plan(desc, true);
     if (ws_bytes < p.total) return EGERIA_ERR_WORKSPACE_TOO_SMALL;
-    const int64_t tiles = (int64_t)desc->batch * desc->heads * row_tiles(desc);
-    if (tiles > 0x7fffffffLL || keys / 4 + 1 > 0x7fffffffLL) return EGERIA_ERR_UNSUPPORTED;
+    if ((rows > keys ? rows : keys) / kRowTile + (int64_t)desc->batch * desc->heads > (1 << 28)) return EGERIA_ERR_UNSUPPORTED;
     AttnArgs a = make_args(desc);
     a.d_o = view_of(dout), a.q = view_of(q), a.k = view_of(k), a.v = view_of(v), a.o = view_of(out);
     a.dq = view_of(dq), a.dk = view_of(dk), a.dv = view_of(dv);
@@ -330,10 +199,9 @@ egeria_status egeria_attention_backward(const egeria_attention_desc *desc, const
     a.delta = (float *)((char *)ws + p.off_delta);
     a.partials = dtable ? (float *)((char *)ws + p.off_part) : nullptr;
     hipStream_t st = (hipStream_t)stream;
-    const bool f32 = desc->dtype == EGERIA_F32;
-    auto go = [&](auto kernel, int64_t blocks) { return launch_k(EGERIA_KERNEL_ATTENTION, kernel, dim3((unsigned)blocks), dim3(256), 0, st, a); };
-    if (tiles > 0) EG_HIP(f32 ? go(attention_dq_kernel<float>, tiles) : go(attention_dq_kernel<uint16_t>, tiles));
-    if (keys > 0) EG_HIP(f32 ? go(attention_dkv_kernel<float>, (keys + 3) / 4) : go(attention_dkv_kernel<uint16_t>, (keys + 3) / 4));
+    bool vec = true;
+    for (const egeria_heads *t : {dout, q, k, v, out, dq, dk, dv}) vec = vec && wide_rows(t, desc);
+    EG_HIP(launch_attention_backward(a, (egeria_dtype)desc->dtype, vec, st));
     if (dtable) EG_HIP(launch_table_reduce(a.partials, a.heads, (int64_t)a.batch * row_tiles(desc), a.table_rows, dtable, st));
     return EGERIA_OK;
 }

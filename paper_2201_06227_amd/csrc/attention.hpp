@@ -33,6 +33,15 @@ hipError_t launch_attention_forward(const AttnArgs &a, egeria_dtype dt, bool vec
 // few rows: a.splits workgroups share a row tile's keys; more than one leaves partial results (split_o, split_ml) that a second
 // launch joins
 hipError_t launch_attention_few(const AttnArgs &a, egeria_dtype dt, bool vec, hipStream_t st);
+// dq, delta and the partial sums of the table's gradient; then dk and dv
+hipError_t launch_attention_backward(const AttnArgs &a, egeria_dtype dt, bool vec, hipStream_t st);
+
+// a launcher's instance for the type, the head size and how the rows are read
+#define EG_PICK(go, a, dt, vec, st)                                                                              \
+    (dt == EGERIA_F32 ? (a.dim <= 64 ? (vec ? go<float, 64, true>(a, st) : go<float, 64, false>(a, st))            \
+                                     : (vec ? go<float, 128, true>(a, st) : go<float, 128, false>(a, st)))         \
+                      : (a.dim <= 64 ? (vec ? go<uint16_t, 64, true>(a, st) : go<uint16_t, 64, false>(a, st))      \
+                                     : (vec ? go<uint16_t, 128, true>(a, st) : go<uint16_t, 128, false>(a, st))))
 
 #ifdef __HIPCC__
 
@@ -69,6 +78,22 @@ __device__ __forceinline__ v16f mma(const v8f &a, const v8f &b, v16f c)
 #pragma unroll
     for (int e = 0; e < 8; ++e) c = __builtin_amdgcn_mfma_f32_32x32x2f32(a.v[e], b.v[e], c, 0, 0, 0);
     return c;
+}
+
+// sum of the lane's products
+__device__ __forceinline__ float dot(v8bf a, v8bf b)
+{
+    float s = 0.0f;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) s = fmaf((float)a[e], (float)b[e], s);
+    return s;
+}
+__device__ __forceinline__ float dot(const v8f &a, const v8f &b)
+{
+    float s = 0.0f;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) s = fmaf(a.v[e], b.v[e], s);
+    return s;
 }
 
 // A 32 x 32 result holds, in register r of lane l, row 8 (r / 4) + 4 (l / 32) + r % 4 of column l % 32.  Registers 8 s ... 8 s + 7 are

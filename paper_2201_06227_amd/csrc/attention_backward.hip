@@ -1,0 +1,348 @@
+// Attention backward: dq, dk, dv and the gradient of the position table from the saved output and log-sum-exp; the probabilities are
+// recomputed.  Two kernels, each the owner of what it writes, so there are no atomics on results and sums have one order: dq (and the
+// table's partial sums) by rows of queries, dk and dv by rows of keys.  Seven products of 2 * pairs * dim instead of the five that a
+// single kernel with atomic sums would do.
+//
+//   dq:  S^T = K Q^T and dP^T = V dO^T (queries across, as in the forward pass), ds = p (dP - D), dQ^T += K^T dS^T
+//   dkv: S = Q K^T and dP = dO V^T (keys across), dV^T += dO^T P, dK^T += Q^T dS
+// In both, P and dS go from result to operand in registers (pack).
+#include "attention.hpp"
+
+namespace egeria {
+
+namespace {
+
+// Keys of a step of the dq kernel: half as many where a step would leave no LDS for the sums by distance.
+template <typename T, int D>
+constexpr int dq_keys() { return sizeof(T) * D == 512 ? kKeyTile / 2 : kKeyTile; }
+
+// ---- dq ---------------------------------------------------------------------------------------------------------
+
+template <typename T, int D, bool VEC>
+__global__ __launch_bounds__(256, sizeof(T) * D == 512 ? 1 : 2) void attention_dq_kernel(AttnArgs a)
+{
+    extern __shared__ __attribute__((aligned(16))) char smem[];
+    typedef Tile<T, D> tile;
+    constexpr int kKeys = dq_keys<T, D>(), kTileBytes = kKeys * tile::kRowBytes;
+    const int tid = threadIdx.x, lane = tid & 63, half = lane >> 5, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const uint32_t tiles = (uint32_t)(a.q_len + kRowTile - 1) / kRowTile, piece = xcd_piece(blockIdx.x, gridDim.x);
+    const uint32_t rt = tiles - 1 - piece % tiles;                          // the longest rows of a causal head first
+    const int q0 = (int)rt * kRowTile, h = (int)(piece / tiles % (uint32_t)a.heads), b = (int)(piece / tiles / (uint32_t)a.heads);
+    const int nq = clamped(a.q_lens, b, a.q_len), nk = clamped(a.k_lens, b, a.k_len), shift = a.causal ? nk - nq : 0;
+    const int rows = nq - q0 < kRowTile ? nq - q0 : kRowTile;
+    int keys = rows > 0 ? nk : 0;
+    if (a.causal && keys > q0 + rows + shift) keys = q0 + rows + shift;
+    const int steps = keys > 0 ? (keys + kKeys - 1) / kKeys : 0;
+
+    const uint32_t lds = (uint32_t)(uintptr_t)(lds_byte *)smem;
+    const int lut_hi = a.b.both ? a.b.far : 0, entries = a.b.far + lut_hi + 1;
+    float *lut = (float *)(smem + 4 * kTileBytes);                          // the bias by distance
+    float *sums = lut + entries;                                            // [wave][half]: sums of ds by distance
+    if (a.table)
+        for (int i = tid; i < entries; i += 256) lut[i] = table_value(a.table, bucket_of_entry(a.b, i), a.heads, h);
+    if (a.partials)
+        for (int i = tid; i < 8 * entries; i += 256) sums[i] = 0.0f;
+    float *mine = sums + (2 * wave + half) * entries;
+
+    Rows<T, D, VEC> qr, kr, vr, gr, orow;
+    qr.open(a.q, b, h, nq, a.dim);
+    gr.open(a.d_o, b, h, nq, a.dim);
+    orow.open(a.o, b, h, nq, a.dim);
+    kr.open(a.k, b, h / a.group, nk, a.dim);
+    vr.open(a.v, b, h / a.group, nk, a.dim);
+    if (steps > 0) {
+        kr.template stage<kKeys, 256>(lds, 0, tid);
+        vr.template stage<kKeys, 256>(lds + kTileBytes, 0, tid);
+    }
+    const int qw = q0 + 32 * wave, i = qw + (lane & 31);
+    const int64_t row = ((int64_t)b * a.heads + h) * a.q_len + i;
+    typename tile::frag q[D / 16], g[D / 16];
+    float delta = 0.0f;
+#pragma unroll
+    for (int kk = 0; kk < D / 16; ++kk) {
+        q[kk] = qr.frag(qw, kk, lane);
+        g[kk] = gr.frag(qw, kk, lane);
+        delta += dot(g[kk], orow.frag(qw, kk, lane));
+    }
+    delta += lane_xor<32>(delta);
+    if (half == 0 && i < a.q_len) a.delta[row] = delta;
+    const float lse = i < nq ? a.lse[row] : -INFINITY;
+    const float base = lse == -INFINITY ? INFINITY : lse * kLog2e, c = a.scale * kLog2e;
+    v16f dq[D / 32];
+#pragma unroll
+    for (int n = 0; n < D / 32; ++n) dq[n] = v16f(0.0f);
+    float left = 0.0f, right = 0.0f;                                        // sums of ds beyond the table by distance
+
+    for (int step = 0; step < steps; ++step) {
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+        __syncthreads();
+        const uint32_t now = lds + (step & 1) * 2 * kTileBytes, next = lds + (~step & 1) * 2 * kTileBytes;
+        const int j0 = step * kKeys;
+        if (step + 1 < steps) {
+            kr.template stage<kKeys, 256>(next, j0 + kKeys, tid);
+            vr.template stage<kKeys, 256>(next + kTileBytes, j0 + kKeys, tid);
+        }
+        if (qw >= nq) continue;
+#pragma unroll
+        for (int n = 0; n < kKeys / 32; ++n) {
+            const int jn = j0 + 32 * n;
+            if (jn >= nk || (a.causal && jn > qw + 31 + shift)) break;      // no pair of the wave is visible
+            v16f s = v16f(0.0f), d = v16f(0.0f);
+#pragma unroll
+            for (int kk = 0; kk < D / 16; ++kk) {
+                s = mma(tile::row_frag(now, 32 * n, kk, lane), q[kk], s);
+                d = mma(tile::row_frag(now + kTileBytes, 32 * n, kk, lane), g[kk], d);
+            }
+            const int lo = jn - (qw + 31) - shift, hi = jn + 31 - qw - shift;             // distances of the wave's pairs
+            const bool edge = jn + 32 > nk || (a.causal && hi > 0);
+            const bool far = !a.table || hi <= -a.b.far || lo >= lut_hi;    // one bias for all of them
+            if (far && !edge) {
+                const float beta = !a.table ? 0.0f : (hi <= -a.b.far ? lut[0] : lut[entries - 1]);
+                const float off = beta - base;
+                float sum = 0.0f;
+#pragma unroll
+                for (int r = 0; r < 16; ++r) {
+                    const float p = __builtin_amdgcn_exp2f(fmaf(s[r], c, off));
+                    s[r] = p * (d[r] - delta);
+                    sum += s[r];
+                }
+                if (hi <= -a.b.far) left += sum;
+                else right += sum;
+            } else {
+                const int rel = jn + 4 * half - i - shift;
+#pragma unroll
+                for (int r = 0; r < 16; ++r) {
+                    const int at = rel + row_of(r, 0);
+                    const float beta = a.table ? lut[distance_index(a.b, at)] : 0.0f;
+                    const bool seen = jn + 4 * half + row_of(r, 0) < nk && (!a.causal || at <= 0);
+                    const float p = __builtin_amdgcn_exp2f(fmaf(s[r], c, beta) - base);
+                    s[r] = seen && p > 0.0f ? p * (d[r] - delta) : 0.0f;
+                    if (a.partials) {
+                        // the 32 lanes of a half have 32 different distances, and the halves tables of their own: no two lanes
+                        // add to one word, and a wave's additions are in order
+                        if (at <= -a.b.far) left += s[r];
+                        else if (at >= lut_hi) right += s[r];
+                        else __hip_atomic_fetch_add(&mine[at + a.b.far], s[r], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
+                    }
+                }
+            }
+#pragma unroll
+            for (int k = 0; k < 2; ++k) {
+                const typename tile::frag f = pack<T>(s, k);
+#pragma unroll
+                for (int m = 0; m < D / 32; ++m) dq[m] = mma(tile::col_frag(now, 32 * n + 16 * k, m, lane), f, dq[m]);
+            }
+        }
+    }
+
+    if (i < a.q_len) {
+        T *out = (T *)a.dq.p + ((int64_t)b * a.dq.sb + (int64_t)i * a.dq.st + (int64_t)h * a.dq.sh);
+        const float k = i < nq ? a.scale : 0.0f;
+#pragma unroll
+        for (int n = 0; n < D / 32; ++n)
+#pragma unroll
+            for (int r = 0; r < 16; r += 4)
+                store4<T, VEC>(out, 32 * n + row_of(r, half), a.dim, dq[n][r] * k, dq[n][r + 1] * k, dq[n][r + 2] * k, dq[n][r + 3] * k);
+    }
+    if (a.partials) {
+        left = wave_sum(left);
+        right = wave_sum(right);
+        __syncthreads();
+        if (lane == 0) {
+            mine[0] += left;                                               // the ends have the same buckets as what lies beyond
+            mine[entries - 1] += right;
+        }
+        __syncthreads();
+        // a bucket for each group of four lanes
+        for (int n = tid >> 2; n < a.table_rows; n += 64) {
+            int count;
+            const int at = entries_of_bucket(a.b, n, &count);
+            float s = 0.0f;
+            for (int e = tid & 3; e < count; e += 4)
+#pragma unroll
+                for (int w = 0; w < 8; ++w) s += sums[w * entries + at + e];
+            s += lane_xor<1>(s);
+            s += lane_xor<2>(s);
+            if ((tid & 3) == 0) a.partials[(((int64_t)h * a.batch + b) * tiles + rt) * a.table_rows + n] = s;
+        }
+    }
+}
+
+// ---- dk, dv -------------------------------------------------------------------------------------------------------
+
+template <typename T, int D, bool VEC>
+__global__ __launch_bounds__(256, sizeof(T) * D == 512 ? 1 : 2) void attention_dkv_kernel(AttnArgs a)
+{
+    extern __shared__ __attribute__((aligned(16))) char smem[];
+    __shared__ float stat[2][2][kKeyTile];                                  // base-2 log-sum-exp and delta of a step's queries
+    typedef Tile<T, D> tile;
+    constexpr int kTileBytes = kKeyTile * tile::kRowBytes;
+    const int tid = threadIdx.x, lane = tid & 63, half = lane >> 5, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const uint32_t tiles = (uint32_t)(a.k_len + kRowTile - 1) / kRowTile, piece = xcd_piece(blockIdx.x, gridDim.x);
+    const int k0 = (int)(piece % tiles) * kRowTile, hk = (int)(piece / tiles % (uint32_t)a.kv_heads), b = (int)(piece / tiles / (uint32_t)a.kv_heads);
+    const int nq = clamped(a.q_lens, b, a.q_len), nk = clamped(a.k_lens, b, a.k_len), shift = a.causal ? nk - nq : 0;
+    // queries that see a key of the tile: from `first` on; the same for every head of the group
+    int first = a.causal && k0 > shift ? (k0 - shift) / kKeyTile * kKeyTile : 0;
+    const int per_head = k0 < nk && first < nq ? (nq - first + kKeyTile - 1) / kKeyTile : 0;
+    const int steps = per_head * a.group;
+
+    const uint32_t lds = (uint32_t)(uintptr_t)(lds_byte *)smem;
+    const int lut_hi = a.b.both ? a.b.far : 0, entries = a.b.far + lut_hi + 1;
+    float *lut = (float *)(smem + 4 * kTileBytes);
+    const int jw = k0 + 32 * wave, j = jw + (lane & 31);
+    const float c = a.scale * kLog2e;
+    Rows<T, D, VEC> kr, vr;
+    kr.open(a.k, b, hk, nk, a.dim);
+    vr.open(a.v, b, hk, nk, a.dim);
+    typename tile::frag k[D / 16], v[D / 16];
+    v16f dk[D / 32], dv[D / 32];
+#pragma unroll
+    for (int n = 0; n < D / 32; ++n) dk[n] = dv[n] = v16f(0.0f);
+
+    // stages the queries of a step: rows into LDS, statistics into registers (the caller stores them once the step before is done)
+    float next_base = 0.0f, next_delta = 0.0f;
+    auto stage = [&](int step) {
+        const int h = hk * a.group + step / per_head, i0 = first + step % per_head * kKeyTile;
+        const uint32_t to = lds + (step & 1) * 2 * kTileBytes;
+        Rows<T, D, VEC> qr, gr;
+        qr.open(a.q, b, h, nq, a.dim);
+        gr.open(a.d_o, b, h, nq, a.dim);
+        qr.template stage<kKeyTile, 256>(to, i0, tid);
+        gr.template stage<kKeyTile, 256>(to + kTileBytes, i0, tid);
+        if (tid < kKeyTile) {
+            const int i = i0 + tid < nq ? i0 + tid : nq - 1;
+            const int64_t row = ((int64_t)b * a.heads + h) * a.q_len + i;
+            next_base = a.lse[row];
+            next_delta = a.delta[row];
+            if (i0 + tid >= nq) next_base = -INFINITY;
+        }
+    };
+    auto keep = [&](int step) {
+        if (tid < kKeyTile) {
+            stat[step & 1][0][tid] = next_base == -INFINITY ? INFINITY : next_base * kLog2e;
+            stat[step & 1][1][tid] = next_delta;
+        }
+    };
+    if (steps > 0) {
+        stage(0);
+        keep(0);
+#pragma unroll
+        for (int kk = 0; kk < D / 16; ++kk) {
+            k[kk] = kr.frag(jw, kk, lane);
+            v[kk] = vr.frag(jw, kk, lane);
+        }
+    }
+    int lut_head = -1;
+    for (int step = 0; step < steps; ++step) {
+        const int h = hk * a.group + step / per_head, i0 = first + step % per_head * kKeyTile;
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+        __syncthreads();
+        if (a.table && h != lut_head) {                                     // the next head of the group
+            for (int n = tid; n < entries; n += 256) lut[n] = table_value(a.table, bucket_of_entry(a.b, n), a.heads, h);
+            lut_head = h;
+            __syncthreads();
+        }
+        const uint32_t now = lds + (step & 1) * 2 * kTileBytes;
+        if (step + 1 < steps) stage(step + 1);
+#pragma unroll
+        for (int n = 0; n < 2; ++n) {
+            const int in = i0 + 32 * n;
+            if (in >= nq || jw >= nk || (a.causal && jw > in + 31 + shift)) continue;
+            v16f s = v16f(0.0f), d = v16f(0.0f);
+#pragma unroll
+            for (int kk = 0; kk < D / 16; ++kk) {
+                s = mma(tile::row_frag(now, 32 * n, kk, lane), k[kk], s);
+                d = mma(tile::row_frag(now + kTileBytes, 32 * n, kk, lane), v[kk], d);
+            }
+            float base[16], delta[16];
+#pragma unroll
+            for (int r = 0; r < 16; r += 4) {
+                *(float4 *)&base[r] = *(const float4 *)&stat[step & 1][0][32 * n + row_of(r, half)];
+                *(float4 *)&delta[r] = *(const float4 *)&stat[step & 1][1][32 * n + row_of(r, half)];
+            }
+            const int lo = jw - (in + 31) - shift, hi = jw + 31 - in - shift;             // distances of the wave's pairs
+            const bool edge = a.causal && hi > 0;
+            const bool far = !a.table || hi <= -a.b.far || lo >= lut_hi;
+            v16f p;
+            if (far && !edge) {
+                const float beta = !a.table ? 0.0f : (hi <= -a.b.far ? lut[0] : lut[entries - 1]);
+#pragma unroll
+                for (int r = 0; r < 16; ++r) {
+                    p[r] = __builtin_amdgcn_exp2f(fmaf(s[r], c, beta - base[r]));
+                    s[r] = p[r] * (d[r] - delta[r]);
+                }
+            } else {
+                const int rel = j - in - 4 * half - shift;
+#pragma unroll
+                for (int r = 0; r < 16; ++r) {
+                    const int at = rel - row_of(r, 0);
+                    const float beta = a.table ? lut[distance_index(a.b, at)] : 0.0f;
+                    const float e = __builtin_amdgcn_exp2f(fmaf(s[r], c, beta) - base[r]);
+                    p[r] = a.causal && at > 0 ? 0.0f : e;
+                    s[r] = p[r] > 0.0f ? p[r] * (d[r] - delta[r]) : 0.0f;
+                }
+            }
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+                const typename tile::frag fp = pack<T>(p, e), fs = pack<T>(s, e);
+#pragma unroll
+                for (int m = 0; m < D / 32; ++m) {
+                    dv[m] = mma(tile::col_frag(now + kTileBytes, 32 * n + 16 * e, m, lane), fp, dv[m]);
+                    dk[m] = mma(tile::col_frag(now, 32 * n + 16 * e, m, lane), fs, dk[m]);
+                }
+            }
+        }
+        if (step + 1 < steps) keep(step + 1);
+    }
+
+    if (j < a.k_len) {
+        T *ok = (T *)a.dk.p + ((int64_t)b * a.dk.sb + (int64_t)j * a.dk.st + (int64_t)hk * a.dk.sh);
+        T *ov = (T *)a.dv.p + ((int64_t)b * a.dv.sb + (int64_t)j * a.dv.st + (int64_t)hk * a.dv.sh);
+        const bool live = j < nk;
+#pragma unroll
+        for (int n = 0; n < D / 32; ++n)
+#pragma unroll
+            for (int r = 0; r < 16; r += 4) {
+                const int f = 32 * n + row_of(r, half);
+                float x[4], y[4];
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    x[e] = live ? dk[n][r + e] * a.scale : 0.0f;
+                    y[e] = live ? dv[n][r + e] : 0.0f;
+                }
+                store4<T, VEC>(ok, f, a.dim, x[0], x[1], x[2], x[3]);
+                store4<T, VEC>(ov, f, a.dim, y[0], y[1], y[2], y[3]);
+            }
+    }
+}
+
+template <typename T, int D, bool VEC>
+hipError_t go_backward(const AttnArgs &a, hipStream_t st)
+{
+    static bool done_q[kMaxDevices] = {}, done_kv[kMaxDevices] = {};
+    const size_t stage = 4 * (size_t)kKeyTile * Tile<T, D>::kRowBytes, stage_q = stage / kKeyTile * dq_keys<T, D>(), entries = a.table ? (size_t)distance_entries(a.b) : 0;
+    if (a.batch == 0) return hipSuccess;
+    if (a.q_len > 0) {
+        const size_t lds = stage_q + 4 * entries * (a.partials ? 9 : 1);
+        hipError_t e = allow_lds(attention_dq_kernel<T, D, VEC>, lds, done_q);
+        if (e != hipSuccess) return e;
+        const int64_t blocks = (int64_t)a.batch * a.heads * ((a.q_len + kRowTile - 1) / kRowTile);
+        e = launch_k(EGERIA_KERNEL_ATTENTION, attention_dq_kernel<T, D, VEC>, dim3((unsigned)blocks), dim3(256), lds, st, a);
+        if (e != hipSuccess) return e;
+    }
+    if (a.k_len > 0) {
+        const size_t lds = stage + 4 * entries;
+        hipError_t e = allow_lds(attention_dkv_kernel<T, D, VEC>, lds, done_kv);
+        if (e != hipSuccess) return e;
+        const int64_t blocks = (int64_t)a.batch * a.kv_heads * ((a.k_len + kRowTile - 1) / kRowTile);
+        e = launch_k(EGERIA_KERNEL_ATTENTION, attention_dkv_kernel<T, D, VEC>, dim3((unsigned)blocks), dim3(256), lds, st, a);
+        if (e != hipSuccess) return e;
+    }
+    return hipSuccess;
+}
+
+}  // namespace
+
+hipError_t launch_attention_backward(const AttnArgs &a, egeria_dtype dt, bool vec, hipStream_t st) { return EG_PICK(go_backward, a, dt, vec, st); }
+
+}  // namespace egeria

@@ -401,13 +401,6 @@ hipError_t go_few(const AttnArgs &a, hipStream_t st)
                     (uint32_t)tiles);
 }
 
-// a launcher's instance for the type, the head size and how the rows are read
-#define EG_PICK(go, a, dt, vec, st)                                                                              \
-    (dt == EGERIA_F32 ? (a.dim <= 64 ? (vec ? go<float, 64, true>(a, st) : go<float, 64, false>(a, st))            \
-                                     : (vec ? go<float, 128, true>(a, st) : go<float, 128, false>(a, st)))         \
-                      : (a.dim <= 64 ? (vec ? go<uint16_t, 64, true>(a, st) : go<uint16_t, 64, false>(a, st))      \
-                                     : (vec ? go<uint16_t, 128, true>(a, st) : go<uint16_t, 128, false>(a, st))))
-
 }  // namespace
 
 hipError_t launch_attention_forward(const AttnArgs &a, egeria_dtype dt, bool vec, hipStream_t st) { return EG_PICK(go, a, dt, vec, st); }
