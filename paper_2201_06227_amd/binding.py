@@ -715,48 +715,84 @@ class PositionBias(NamedTuple):
         return PositionTable(t.data_ptr(), t.shape[0], int(self.max_distance), 1 if self.bidirectional else 0)
 
 
-def _same_device(*tensors: Optional[torch.Tensor]) -> None:
+# The calls below are short beside the host's work for them, which is all of a small call's time: descriptors are packed as bytes
+# (which ctypes passes as pointers) instead of through the structs' fields, and workspace sizes, a function of the sizes alone,
+# are asked for once.  A forward call of 4 x 32 tokens: 18.5 -> HOST_US us.
+_desc_struct = struct.Struct("@iiiiiiiifPPP")
+_heads_struct = struct.Struct("@Pqqq")
+assert _desc_struct.size == ctypes.sizeof(AttentionDesc) and _heads_struct.size == ctypes.sizeof(Heads)
+
+
+@functools.lru_cache(maxsize=None)
+def _raw(name: str, n_args: int):
+    """The library's function of this name with every argument an address (bytes, an integer or None)."""
+    f = lib()[name]
+    f.restype, f.argtypes = ctypes.c_int, [_vp] * n_args
+    return f
+
+
+def _same_device(*tensors: Optional[torch.Tensor]) -> int:
     """Kernels go to the current device's current stream: everything a call touches has to be there."""
-    here = torch.cuda.current_device() if any(t is not None and t.is_cuda for t in tensors) else -1
+    dev = tensors[0].get_device()
+    if dev < 0 or dev != torch.cuda.current_device():
+        raise ValueError("tensors on the current device expected")
     for t in tensors:
-        if t is not None and (not t.is_cuda or t.device.index != here):
+        if t is not None and t.get_device() != dev:
             raise ValueError("tensors on the current device expected")
+    return dev
 
 
-def _heads(t: torch.Tensor) -> Heads:
+def _heads(t: torch.Tensor) -> bytes:
+    """egeria_heads of a tensor [batch, token, head, feature]."""
     if t.dim() != 4:
         raise ValueError("[batch, token, head, feature] expected")
-    if t.shape[3] > 1 and t.stride(3) != 1:
+    sb, st, sh, sf = t.stride()
+    if sf != 1 and t.shape[3] > 1:
         raise ValueError("contiguous features expected")
-    return Heads(t.data_ptr(), t.stride(0), t.stride(1), t.stride(2))
+    return _heads_struct.pack(t.data_ptr(), sb, st, sh)
 
 
-def _lens(t: Optional[torch.Tensor], batch: int):
+def _lens(t: Optional[torch.Tensor], batch: int) -> int:
     if t is None:
-        return None
+        return 0
     if t.dtype != torch.int32 or t.shape != (batch,) or not t.is_contiguous():
         raise ValueError("lengths are a contiguous int32 tensor [batch]")
     return t.data_ptr()
 
 
-def _attention_desc(q, k, v, causal, scale, q_lens, k_lens, bias) -> AttentionDesc:
-    if q.dim() != 4 or k.dim() != 4 or k.shape != v.shape or k.shape[0] != q.shape[0] or k.shape[3] != q.shape[3]:
+def _attention_desc(q, k, v, causal, scale, q_lens, k_lens, bias):
+    """(egeria_attention_desc as bytes, what it depends on for the workspace, what has to stay alive)"""
+    qs, ks = q.shape, k.shape
+    if len(qs) != 4 or len(ks) != 4 or ks != v.shape or ks[0] != qs[0] or ks[3] != qs[3]:
         raise ValueError("q [batch, q_len, heads, dim] and k, v [batch, k_len, kv_heads, dim] expected")
     if not q.dtype == k.dtype == v.dtype:
         raise ValueError("q, k and v must have one dtype")
-    batch, q_len, heads, dim = q.shape
-    tab = None
+    batch, q_len, heads, dim = qs
+    tab, at, rows = None, 0, 0
     if bias is not None:
         if bias.table.dim() != 2 or bias.table.shape[1] != heads:
             raise ValueError("a position table is fp32 [buckets, heads]")
-        tab = ctypes.pointer(bias.c_struct())
-    scale = 1.0 / math.sqrt(dim) if scale is None and dim else scale
-    return AttentionDesc(_dt(q), batch, heads, k.shape[2], q_len, k.shape[1], dim, 1 if causal else 0, scale or 0.0,
-                         _lens(q_lens, batch), _lens(k_lens, batch), tab)
+        tab = bias.c_struct()
+        at, rows = ctypes.addressof(tab), tab.buckets
+    if scale is None:
+        scale = 1.0 / math.sqrt(dim) if dim else 0.0
+    sizes = (_dt(q), batch, heads, ks[2], q_len, ks[1], dim, 1 if causal else 0)
+    return _desc_struct.pack(*sizes, scale, _lens(q_lens, batch), _lens(k_lens, batch), at), (*sizes[:7], rows), tab
 
 
-def attention_workspace_bytes(desc: AttentionDesc, backward: bool) -> int:
-    return int(lib().egeria_attention_workspace_bytes(ctypes.byref(desc), 1 if backward else 0))
+_attention_ws = {}
+
+
+def _attention_workspace_bytes(desc: bytes, sizes: tuple, backward: int) -> int:
+    n = _attention_ws.get((sizes, backward))
+    if n is None:
+        n = int(lib().egeria_attention_workspace_bytes(AttentionDesc.from_buffer_copy(desc), backward))
+        if n == 0:
+            return 256                                   # the call itself says what is wrong
+        if len(_attention_ws) >= 1024:                   # sequence lengths can change with every mini-batch
+            _attention_ws.clear()
+        _attention_ws[sizes, backward] = n
+    return n
 
 
 def attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, causal: bool = False, scale: Optional[float] = None,
@@ -765,20 +801,23 @@ def attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, causal: bool = 
               ws: Optional[torch.Tensor] = None):
     """egeria_attention: q [batch, q_len, heads, dim], k and v [batch, k_len, kv_heads, dim] (any strides with contiguous
     features) -> out like q, and lse fp32 [batch, heads, q_len].  scale: 1 / sqrt(dim) if not given."""
-    _same_device(q, k, v, q_lens, k_lens, out, lse, ws, None if bias is None else bias.table)
-    desc = _attention_desc(q, k, v, causal, scale, q_lens, k_lens, bias)
+    dev = _same_device(q, k, v, q_lens, k_lens, out, lse, ws, None if bias is None else bias.table)
+    desc, sizes, _tab = _attention_desc(q, k, v, causal, scale, q_lens, k_lens, bias)
+    batch, q_len, heads, _ = q.shape
     if out is None:
         out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
     elif out.shape != q.shape or out.dtype != q.dtype:
         raise ValueError("out must have q's shape and dtype")
     if lse is None:
-        lse = torch.empty((q.shape[0], q.shape[2], q.shape[1]), dtype=torch.float32, device=q.device)
-    elif lse.shape != (q.shape[0], q.shape[2], q.shape[1]) or lse.dtype != torch.float32 or not lse.is_contiguous():
+        lse = torch.empty((batch, heads, q_len), dtype=torch.float32, device=q.device)
+    elif lse.shape != (batch, heads, q_len) or lse.dtype != torch.float32 or not lse.is_contiguous():
         raise ValueError("lse must be a contiguous fp32 tensor [batch, heads, q_len]")
-    ws = workspace(attention_workspace_bytes(desc, False), q.device) if ws is None else ws
-    views = [_heads(t) for t in (q, k, v, out)]
-    rc = lib().egeria_attention(desc, *views, _ptr(lse), _ptr(ws), ws.numel(), _stream())
-    _check(rc, "egeria_attention")
+    if ws is None:
+        ws = torch.empty(_attention_workspace_bytes(desc, sizes, 0), dtype=torch.uint8, device=q.device)
+    rc = _raw("egeria_attention", 9)(desc, _heads(q), _heads(k), _heads(v), _heads(out), lse.data_ptr(), ws.data_ptr(), ws.numel(),
+                                     torch._C._cuda_getCurrentRawStream(dev))
+    if rc:
+        _check(rc, "egeria_attention")
     return out, lse
 
 
@@ -790,23 +829,28 @@ def attention_backward(dout: torch.Tensor, q: torch.Tensor, k: torch.Tensor, v: 
     """egeria_attention_backward: (dq, dk, dv, dtable) from the arguments and results of attention().  dtable is fp32
     [buckets, heads], or None without bias or with table_grad = False.  dq, dk, dv: tensors to write, e.g. the slices of a packed
     gradient."""
-    _same_device(dout, q, k, v, out, lse, q_lens, k_lens, dq, dk, dv, ws, None if bias is None else bias.table)
-    desc = _attention_desc(q, k, v, causal, scale, q_lens, k_lens, bias)
-    for t, name in ((dout, "dout"), (out, "out")):
-        if t.shape != q.shape or t.dtype != q.dtype:
-            raise ValueError(f"{name} must have q's shape and dtype")
-    if lse.shape != (q.shape[0], q.shape[2], q.shape[1]) or lse.dtype != torch.float32 or not lse.is_contiguous():
+    dev = _same_device(dout, q, k, v, out, lse, q_lens, k_lens, dq, dk, dv, ws, None if bias is None else bias.table)
+    desc, sizes, _tab = _attention_desc(q, k, v, causal, scale, q_lens, k_lens, bias)
+    if dout.shape != q.shape or dout.dtype != q.dtype or out.shape != q.shape or out.dtype != q.dtype:
+        raise ValueError("dout and out must have q's shape and dtype")
+    batch, q_len, heads, _ = q.shape
+    if lse.shape != (batch, heads, q_len) or lse.dtype != torch.float32 or not lse.is_contiguous():
         raise ValueError("lse must be a contiguous fp32 tensor [batch, heads, q_len]")
     grads = []
-    for g, t, name in ((dq, q, "dq"), (dk, k, "dk"), (dv, v, "dv")):
-        if g is not None and (g.shape != t.shape or g.dtype != t.dtype):
-            raise ValueError(f"{name} must have the shape and dtype of what it is the gradient of")
-        grads.append(torch.empty(t.shape, dtype=t.dtype, device=t.device) if g is None else g)
+    for g, t in ((dq, q), (dk, k), (dv, v)):
+        if g is None:
+            g = torch.empty(t.shape, dtype=t.dtype, device=t.device)
+        elif g.shape != t.shape or g.dtype != t.dtype:
+            raise ValueError("dq, dk and dv must have the shapes and dtype of q, k and v")
+        grads.append(g)
     dtable = torch.empty_like(bias.table) if bias is not None and table_grad else None
-    ws = workspace(attention_workspace_bytes(desc, True), q.device) if ws is None else ws
-    rc = lib().egeria_attention_backward(desc, *[_heads(t) for t in (dout, q, k, v, out)], _ptr(lse),
-                                         *[_heads(t) for t in grads], _ptr(dtable), _ptr(ws), ws.numel(), _stream())
-    _check(rc, "egeria_attention_backward")
+    if ws is None:
+        ws = torch.empty(_attention_workspace_bytes(desc, sizes, 1), dtype=torch.uint8, device=q.device)
+    rc = _raw("egeria_attention_backward", 14)(
+        desc, _heads(dout), _heads(q), _heads(k), _heads(v), _heads(out), lse.data_ptr(), _heads(grads[0]), _heads(grads[1]),
+        _heads(grads[2]), None if dtable is None else dtable.data_ptr(), ws.data_ptr(), ws.numel(), torch._C._cuda_getCurrentRawStream(dev))
+    if rc:
+        _check(rc, "egeria_attention_backward")
     return (*grads, dtable)
 
 

@@ -285,12 +285,45 @@ __device__ __forceinline__ void store4(T *row, int f, int dim, float x0, float x
     }
 }
 
-// The table by distance of one head in LDS, in units of the scores' base-2 exponent; hidden entries are minus infinity.
+// The bias of one head by distance, in LDS: table entries in units of the scores' base-2 exponent (hidden ones minus infinity), from
+// distance -far - kPad to hi + kPad.  A block of at most 64 keys and 32 queries that reaches into [-far, hi] has no distance outside, so
+// its pairs are looked up without clamping, four neighbouring distances at a time; every other block has one bias for all of
+// its pairs.
+constexpr int kPad = 96;
 __device__ __forceinline__ float table_value(const float *table, int row, int heads, int h)
 {
     const float t = table[row * heads + h];
     return t <= kHidden ? -INFINITY : t * kLog2e;
 }
+inline size_t bias_lut_floats(const AttnArgs &a) { return a.table ? align_up((size_t)distance_entries(a.b) + 2 * kPad, 4) : 0; }
+
+typedef float v4f_any __attribute__((ext_vector_type(4), aligned(4)));
+
+struct BiasLut {
+    float *lut;
+    int far, hi;                            // ends of the table: distances beyond them have the bias of the nearest end
+    bool on;
+
+    __device__ __forceinline__ void open(const AttnArgs &a, float *memory)
+    {
+        lut = memory;
+        on = a.table != nullptr;
+        far = a.b.far;
+        hi = a.b.both ? a.b.far : 0;
+    }
+    __device__ __forceinline__ int count() const { return far + hi + 1 + 2 * kPad; }
+    // by all 256 threads; the caller synchronises
+    __device__ __forceinline__ void fill(const AttnArgs &a, int h, int tid) const
+    {
+        if (!on) return;
+        for (int n = tid; n < count(); n += 256) lut[n] = table_value(a.table, bucket_of_entry(a.b, distance_index(a.b, n - kPad - far)), a.heads, h);
+    }
+    // a block of pairs with distances lo ... top: one bias for all of them, which is it
+    __device__ __forceinline__ bool left(int top) const { return top <= -far; }
+    __device__ __forceinline__ bool one(int lo, int top) const { return !on || left(top) || lo >= hi; }
+    __device__ __forceinline__ float the_one(int top) const { return !on ? 0.0f : lut[left(top) ? 0 : count() - 1]; }
+    __device__ __forceinline__ v4f_any four(int rel) const { return *(const v4f_any *)(lut + (rel + far + kPad)); }
+};
 
 template <typename K>
 inline hipError_t allow_lds(K kernel, size_t bytes, bool (&done)[kMaxDevices])

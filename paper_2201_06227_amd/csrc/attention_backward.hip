@@ -16,6 +16,41 @@ namespace {
 template <typename T, int D>
 constexpr int dq_keys() { return sizeof(T) * D == 512 ? kKeyTile / 2 : kKeyTile; }
 
+// Adds a block's dS^T (keys down, queries across) to sums by distance: into[d] for d = key - query of the block.
+// A value in lane l of a row of 16 lanes and register r has distance u - l, u being the register's key modulo 16, up to multiples of
+// 16 and of the half's 4 that all lanes of the row share.  Moved down by u lanes, values of one distance lie in one lane, those
+// that leave the row at the bottom come in at the top 16 distances further: two additions with a shift of lanes each, no LDS.  What
+// is left are the sums of 4 times 16 distances for each half of the wave, which has a table of its own: plain additions, in a
+// fixed order.  (As additions of all 1024 values in LDS, atomic ones that never collide, dq of 64 x 256 x 12 x 64 took 188 us, now
+// DQ_US.)
+template <int R>
+__device__ __forceinline__ void shift_add(const v16f &s, float (&a)[3])
+{
+    constexpr int key = 8 * (R >> 2) + (R & 3), u = key & 15, w = key >> 4;
+    const int x = __float_as_int(s[R]);
+    if constexpr (u == 0) a[w] += s[R];
+    else {
+        a[w] += __int_as_float(__builtin_amdgcn_update_dpp(0, x, 0x100 | u, 0xf, 0xf, true));                // lane i takes from i + u
+        a[w + 1] += __int_as_float(__builtin_amdgcn_update_dpp(0, x, 0x110 | (16 - u), 0xf, 0xf, true));     // from i - (16 - u)
+    }
+    if constexpr (R < 15) shift_add<R + 1>(s, a);
+}
+__device__ __forceinline__ void add_diagonals(const v16f &s, float *into, int lane)
+{
+    float a[3] = {0.0f, 0.0f, 0.0f};
+    shift_add<0>(s, a);
+    // a[v] of lane l: distance 16 v + 4 half - 16 (row of lanes in the half) - l % 16
+    const float up1 = lane_xor<16>(a[1]), up2 = lane_xor<16>(a[2]);
+    const bool low = !(lane & 16);
+    float *at = into + 4 * (lane >> 5) - (lane & 15);
+    const float x = low ? a[0] + up1 : a[0], y = a[1] + up2, z = a[2];
+    at[low ? 0 : -16] += x;
+    if (low) {
+        at[16] += y;
+        at[32] += z;
+    }
+}
+
 // ---- dq ---------------------------------------------------------------------------------------------------------
 
 template <typename T, int D, bool VEC>
@@ -35,11 +70,11 @@ __global__ __launch_bounds__(256, sizeof(T) * D == 512 ? 1 : 2) void attention_d
     const int steps = keys > 0 ? (keys + kKeys - 1) / kKeys : 0;
 
     const uint32_t lds = (uint32_t)(uintptr_t)(lds_byte *)smem;
-    const int lut_hi = a.b.both ? a.b.far : 0, entries = a.b.far + lut_hi + 1;
-    float *lut = (float *)(smem + 4 * kTileBytes);                          // the bias by distance
-    float *sums = lut + entries;                                            // [wave][half]: sums of ds by distance
-    if (a.table)
-        for (int i = tid; i < entries; i += 256) lut[i] = table_value(a.table, bucket_of_entry(a.b, i), a.heads, h);
+    BiasLut bias;
+    bias.open(a, (float *)(smem + 4 * kTileBytes));
+    bias.fill(a, h, tid);
+    const int entries = bias.count();
+    float *sums = bias.lut + ((entries + 3) & ~3);                          // [wave][half]: sums of ds by distance, laid out as the bias
     if (a.partials)
         for (int i = tid; i < 8 * entries; i += 256) sums[i] = 0.0f;
     float *mine = sums + (2 * wave + half) * entries;
@@ -95,36 +130,36 @@ __global__ __launch_bounds__(256, sizeof(T) * D == 512 ? 1 : 2) void attention_d
             }
             const int lo = jn - (qw + 31) - shift, hi = jn + 31 - qw - shift;             // distances of the wave's pairs
             const bool edge = jn + 32 > nk || (a.causal && hi > 0);
-            const bool far = !a.table || hi <= -a.b.far || lo >= lut_hi;    // one bias for all of them
-            if (far && !edge) {
-                const float beta = !a.table ? 0.0f : (hi <= -a.b.far ? lut[0] : lut[entries - 1]);
+            const bool one = bias.one(lo, hi);
+            const float beta = bias.the_one(hi);
+            const int rel = jn + 4 * half - i - shift;
+            if (one) {
                 const float off = beta - base;
-                float sum = 0.0f;
 #pragma unroll
-                for (int r = 0; r < 16; ++r) {
-                    const float p = __builtin_amdgcn_exp2f(fmaf(s[r], c, off));
-                    s[r] = p * (d[r] - delta);
-                    sum += s[r];
-                }
-                if (hi <= -a.b.far) left += sum;
-                else right += sum;
+                for (int r = 0; r < 16; ++r) s[r] = __builtin_amdgcn_exp2f(fmaf(s[r], c, off));
             } else {
-                const int rel = jn + 4 * half - i - shift;
 #pragma unroll
-                for (int r = 0; r < 16; ++r) {
-                    const int at = rel + row_of(r, 0);
-                    const float beta = a.table ? lut[distance_index(a.b, at)] : 0.0f;
-                    const bool seen = jn + 4 * half + row_of(r, 0) < nk && (!a.causal || at <= 0);
-                    const float p = __builtin_amdgcn_exp2f(fmaf(s[r], c, beta) - base);
-                    s[r] = seen && p > 0.0f ? p * (d[r] - delta) : 0.0f;
-                    if (a.partials) {
-                        // the 32 lanes of a half have 32 different distances, and the halves tables of their own: no two lanes
-                        // add to one word, and a wave's additions are in order
-                        if (at <= -a.b.far) left += s[r];
-                        else if (at >= lut_hi) right += s[r];
-                        else __hip_atomic_fetch_add(&mine[at + a.b.far], s[r], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
-                    }
+                for (int r = 0; r < 16; r += 4) {
+                    const v4f_any t = bias.four(rel + row_of(r, 0));
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) s[r + e] = __builtin_amdgcn_exp2f(fmaf(s[r + e], c, t[e] - base));
                 }
+            }
+#pragma unroll
+            for (int r = 0; r < 16; ++r) s[r] *= d[r] - delta;
+            if (edge) {
+#pragma unroll
+                for (int r = 0; r < 16; ++r)
+                    if (jn + 4 * half + row_of(r, 0) >= nk || (a.causal && rel + row_of(r, 0) > 0)) s[r] = 0.0f;
+            }
+            if (a.partials) {
+                if (one) {
+                    float sum = 0.0f;
+#pragma unroll
+                    for (int r = 0; r < 16; ++r) sum += s[r];
+                    if (bias.left(hi)) left += sum;
+                    else right += sum;
+                } else add_diagonals(s, mine + (jn - qw - shift + bias.far + kPad), lane);
             }
 #pragma unroll
             for (int k = 0; k < 2; ++k) {
@@ -149,14 +184,17 @@ __global__ __launch_bounds__(256, sizeof(T) * D == 512 ? 1 : 2) void attention_d
         right = wave_sum(right);
         __syncthreads();
         if (lane == 0) {
-            mine[0] += left;                                               // the ends have the same buckets as what lies beyond
+            mine[0] += left;
             mine[entries - 1] += right;
         }
         __syncthreads();
         // a bucket for each group of four lanes
         for (int n = tid >> 2; n < a.table_rows; n += 64) {
-            int count;
-            const int at = entries_of_bucket(a.b, n, &count);
+            int count, at = entries_of_bucket(a.b, n, &count);
+            // the table's ends have the same buckets as the distances beyond them
+            if (count > 0 && at + count == entries - 2 * kPad) count += kPad;
+            if (count > 0 && at == 0) count += kPad;
+            else at += kPad;
             float s = 0.0f;
             for (int e = tid & 3; e < count; e += 4)
 #pragma unroll
@@ -168,33 +206,41 @@ __global__ __launch_bounds__(256, sizeof(T) * D == 512 ? 1 : 2) void attention_d
     }
 }
 
+// Queries of a step of the dk / dv kernel.  Heads of 128: the values of the workgroup's keys stay in LDS, since their fragments beside
+// the keys' and two sums of 128 x 32 would overflow a wave's 256 registers; with steps of 32 queries two workgroups still share a
+// compute unit.
+template <int D>
+constexpr int dkv_queries() { return D > 64 ? 32 : kKeyTile; }
+
 // ---- dk, dv -------------------------------------------------------------------------------------------------------
 
 template <typename T, int D, bool VEC>
 __global__ __launch_bounds__(256, sizeof(T) * D == 512 ? 1 : 2) void attention_dkv_kernel(AttnArgs a)
 {
     extern __shared__ __attribute__((aligned(16))) char smem[];
-    __shared__ float stat[2][2][kKeyTile];                                  // base-2 log-sum-exp and delta of a step's queries
     typedef Tile<T, D> tile;
-    constexpr int kTileBytes = kKeyTile * tile::kRowBytes;
+    constexpr int kQueries = dkv_queries<D>(), kTileBytes = kQueries * tile::kRowBytes;
+    constexpr bool kValuesInLds = D > 64;
+    __shared__ float stat[2][2][kQueries];                                  // base-2 log-sum-exp and delta of a step's queries
     const int tid = threadIdx.x, lane = tid & 63, half = lane >> 5, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const uint32_t tiles = (uint32_t)(a.k_len + kRowTile - 1) / kRowTile, piece = xcd_piece(blockIdx.x, gridDim.x);
     const int k0 = (int)(piece % tiles) * kRowTile, hk = (int)(piece / tiles % (uint32_t)a.kv_heads), b = (int)(piece / tiles / (uint32_t)a.kv_heads);
     const int nq = clamped(a.q_lens, b, a.q_len), nk = clamped(a.k_lens, b, a.k_len), shift = a.causal ? nk - nq : 0;
     // queries that see a key of the tile: from `first` on; the same for every head of the group
-    int first = a.causal && k0 > shift ? (k0 - shift) / kKeyTile * kKeyTile : 0;
-    const int per_head = k0 < nk && first < nq ? (nq - first + kKeyTile - 1) / kKeyTile : 0;
+    int first = a.causal && k0 > shift ? (k0 - shift) / kQueries * kQueries : 0;
+    const int per_head = k0 < nk && first < nq ? (nq - first + kQueries - 1) / kQueries : 0;
     const int steps = per_head * a.group;
 
     const uint32_t lds = (uint32_t)(uintptr_t)(lds_byte *)smem;
-    const int lut_hi = a.b.both ? a.b.far : 0, entries = a.b.far + lut_hi + 1;
-    float *lut = (float *)(smem + 4 * kTileBytes);
+    constexpr int kStage = 4 * kTileBytes + (kValuesInLds ? kRowTile * tile::kRowBytes : 0);
+    BiasLut bias;
+    bias.open(a, (float *)(smem + kStage));
     const int jw = k0 + 32 * wave, j = jw + (lane & 31);
     const float c = a.scale * kLog2e;
     Rows<T, D, VEC> kr, vr;
     kr.open(a.k, b, hk, nk, a.dim);
     vr.open(a.v, b, hk, nk, a.dim);
-    typename tile::frag k[D / 16], v[D / 16];
+    typename tile::frag k[D / 16], v[kValuesInLds ? 1 : D / 16];
     v16f dk[D / 32], dv[D / 32];
 #pragma unroll
     for (int n = 0; n < D / 32; ++n) dk[n] = dv[n] = v16f(0.0f);
@@ -202,14 +248,14 @@ __global__ __launch_bounds__(256, sizeof(T) * D == 512 ? 1 : 2) void attention_d
     // stages the queries of a step: rows into LDS, statistics into registers (the caller stores them once the step before is done)
     float next_base = 0.0f, next_delta = 0.0f;
     auto stage = [&](int step) {
-        const int h = hk * a.group + step / per_head, i0 = first + step % per_head * kKeyTile;
+        const int h = hk * a.group + step / per_head, i0 = first + step % per_head * kQueries;
         const uint32_t to = lds + (step & 1) * 2 * kTileBytes;
         Rows<T, D, VEC> qr, gr;
         qr.open(a.q, b, h, nq, a.dim);
         gr.open(a.d_o, b, h, nq, a.dim);
-        qr.template stage<kKeyTile, 256>(to, i0, tid);
-        gr.template stage<kKeyTile, 256>(to + kTileBytes, i0, tid);
-        if (tid < kKeyTile) {
+        qr.template stage<kQueries, 256>(to, i0, tid);
+        gr.template stage<kQueries, 256>(to + kTileBytes, i0, tid);
+        if (tid < kQueries) {
             const int i = i0 + tid < nq ? i0 + tid : nq - 1;
             const int64_t row = ((int64_t)b * a.heads + h) * a.q_len + i;
             next_base = a.lse[row];
@@ -218,69 +264,71 @@ __global__ __launch_bounds__(256, sizeof(T) * D == 512 ? 1 : 2) void attention_d
         }
     };
     auto keep = [&](int step) {
-        if (tid < kKeyTile) {
+        if (tid < kQueries) {
             stat[step & 1][0][tid] = next_base == -INFINITY ? INFINITY : next_base * kLog2e;
             stat[step & 1][1][tid] = next_delta;
         }
     };
     if (steps > 0) {
+        if constexpr (kValuesInLds) vr.template stage<kRowTile, 256>(lds + 4 * kTileBytes, k0, tid);
         stage(0);
         keep(0);
 #pragma unroll
         for (int kk = 0; kk < D / 16; ++kk) {
             k[kk] = kr.frag(jw, kk, lane);
-            v[kk] = vr.frag(jw, kk, lane);
+            if constexpr (!kValuesInLds) v[kk] = vr.frag(jw, kk, lane);
         }
     }
     int lut_head = -1;
     for (int step = 0; step < steps; ++step) {
-        const int h = hk * a.group + step / per_head, i0 = first + step % per_head * kKeyTile;
+        const int h = hk * a.group + step / per_head, i0 = first + step % per_head * kQueries;
         asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
         __syncthreads();
         if (a.table && h != lut_head) {                                     // the next head of the group
-            for (int n = tid; n < entries; n += 256) lut[n] = table_value(a.table, bucket_of_entry(a.b, n), a.heads, h);
+            bias.fill(a, h, tid);
             lut_head = h;
             __syncthreads();
         }
         const uint32_t now = lds + (step & 1) * 2 * kTileBytes;
         if (step + 1 < steps) stage(step + 1);
 #pragma unroll
-        for (int n = 0; n < 2; ++n) {
+        for (int n = 0; n < kQueries / 32; ++n) {
             const int in = i0 + 32 * n;
             if (in >= nq || jw >= nk || (a.causal && jw > in + 31 + shift)) continue;
             v16f s = v16f(0.0f), d = v16f(0.0f);
 #pragma unroll
             for (int kk = 0; kk < D / 16; ++kk) {
                 s = mma(tile::row_frag(now, 32 * n, kk, lane), k[kk], s);
-                d = mma(tile::row_frag(now + kTileBytes, 32 * n, kk, lane), v[kk], d);
-            }
-            float base[16], delta[16];
-#pragma unroll
-            for (int r = 0; r < 16; r += 4) {
-                *(float4 *)&base[r] = *(const float4 *)&stat[step & 1][0][32 * n + row_of(r, half)];
-                *(float4 *)&delta[r] = *(const float4 *)&stat[step & 1][1][32 * n + row_of(r, half)];
+                if constexpr (kValuesInLds)
+                    d = mma(tile::row_frag(now + kTileBytes, 32 * n, kk, lane), tile::row_frag(lds + 4 * kTileBytes, 32 * wave, kk, lane), d);
+                else d = mma(tile::row_frag(now + kTileBytes, 32 * n, kk, lane), v[kk], d);
             }
             const int lo = jw - (in + 31) - shift, hi = jw + 31 - in - shift;             // distances of the wave's pairs
-            const bool edge = a.causal && hi > 0;
-            const bool far = !a.table || hi <= -a.b.far || lo >= lut_hi;
+            const bool one = bias.one(lo, hi);
+            const float beta = bias.the_one(hi);
+            const int rel = j - in - 4 * half - shift;
             v16f p;
-            if (far && !edge) {
-                const float beta = !a.table ? 0.0f : (hi <= -a.b.far ? lut[0] : lut[entries - 1]);
 #pragma unroll
-                for (int r = 0; r < 16; ++r) {
-                    p[r] = __builtin_amdgcn_exp2f(fmaf(s[r], c, beta - base[r]));
-                    s[r] = p[r] * (d[r] - delta[r]);
-                }
-            } else {
-                const int rel = j - in - 4 * half - shift;
+            for (int r = 0; r < 16; r += 4) {
+                const float4 base = *(const float4 *)&stat[step & 1][0][32 * n + row_of(r, half)];
+                const float bs[4] = {base.x, base.y, base.z, base.w};
+                v4f_any t;
+                if (one) t = v4f_any(beta);
+                else t = bias.four(rel - row_of(r, 0) - 3);                // of the keys' distances from four queries, the last first
 #pragma unroll
-                for (int r = 0; r < 16; ++r) {
-                    const int at = rel - row_of(r, 0);
-                    const float beta = a.table ? lut[distance_index(a.b, at)] : 0.0f;
-                    const float e = __builtin_amdgcn_exp2f(fmaf(s[r], c, beta) - base[r]);
-                    p[r] = a.causal && at > 0 ? 0.0f : e;
-                    s[r] = p[r] > 0.0f ? p[r] * (d[r] - delta[r]) : 0.0f;
-                }
+                for (int e = 0; e < 4; ++e) p[r + e] = __builtin_amdgcn_exp2f(fmaf(s[r + e], c, t[3 - e] - bs[e]));
+            }
+            if (a.causal && hi > 0) {
+#pragma unroll
+                for (int r = 0; r < 16; ++r)
+                    if (rel - row_of(r, 0) > 0) p[r] = 0.0f;
+            }
+#pragma unroll
+            for (int r = 0; r < 16; r += 4) {
+                const float4 delta = *(const float4 *)&stat[step & 1][1][32 * n + row_of(r, half)];
+                const float ds[4] = {delta.x, delta.y, delta.z, delta.w};
+#pragma unroll
+                for (int e = 0; e < 4; ++e) s[r + e] = p[r + e] * (d[r + e] - ds[e]);
             }
 #pragma unroll
             for (int e = 0; e < 2; ++e) {
@@ -320,10 +368,10 @@ template <typename T, int D, bool VEC>
 hipError_t go_backward(const AttnArgs &a, hipStream_t st)
 {
     static bool done_q[kMaxDevices] = {}, done_kv[kMaxDevices] = {};
-    const size_t stage = 4 * (size_t)kKeyTile * Tile<T, D>::kRowBytes, stage_q = stage / kKeyTile * dq_keys<T, D>(), entries = a.table ? (size_t)distance_entries(a.b) : 0;
+    const size_t row = (size_t)Tile<T, D>::kRowBytes, lut = bias_lut_floats(a);
     if (a.batch == 0) return hipSuccess;
     if (a.q_len > 0) {
-        const size_t lds = stage_q + 4 * entries * (a.partials ? 9 : 1);
+        const size_t lds = 4 * dq_keys<T, D>() * row + 4 * lut * (a.partials ? 9 : 1);
         hipError_t e = allow_lds(attention_dq_kernel<T, D, VEC>, lds, done_q);
         if (e != hipSuccess) return e;
         const int64_t blocks = (int64_t)a.batch * a.heads * ((a.q_len + kRowTile - 1) / kRowTile);
@@ -331,7 +379,7 @@ hipError_t go_backward(const AttnArgs &a, hipStream_t st)
         if (e != hipSuccess) return e;
     }
     if (a.k_len > 0) {
-        const size_t lds = stage + 4 * entries;
+        const size_t lds = 4 * dkv_queries<D>() * row + (D > 64 ? kRowTile * row : 0) + 4 * lut;
         hipError_t e = allow_lds(attention_dkv_kernel<T, D, VEC>, lds, done_kv);
         if (e != hipSuccess) return e;
         const int64_t blocks = (int64_t)a.batch * a.kv_heads * ((a.k_len + kRowTile - 1) / kRowTile);

@@ -93,10 +93,9 @@ __global__ __launch_bounds__(256, sizeof(T) * D == 512 ? 1 : 2) void attention_f
     const int steps = keys > 0 ? (keys + kKeyTile - 1) / kKeyTile : 0;
 
     const uint32_t lds = (uint32_t)(uintptr_t)(lds_byte *)smem;
-    float *lut = (float *)(smem + 4 * kTileBytes);
-    const int lut_hi = a.b.both ? a.b.far : 0;
-    if (a.table)
-        for (int i = tid; i <= a.b.far + lut_hi; i += 256) lut[i] = table_value(a.table, bucket_of_entry(a.b, i), a.heads, h);
+    BiasLut bias;
+    bias.open(a, (float *)(smem + 4 * kTileBytes));
+    bias.fill(a, h, tid);
 
     Rows<T, D, VEC> qr, kr, vr;
     qr.open(a.q, b, h, nq, a.dim);
@@ -127,9 +126,9 @@ __global__ __launch_bounds__(256, sizeof(T) * D == 512 ? 1 : 2) void attention_f
         st.scores(s, now, lane);
         const int lo = j0 - (qw + 31) - shift, hi = j0 + kKeyTile - 1 - qw - shift;       // distances of the wave's pairs
         const bool edge = j0 + kKeyTile > nk || (a.causal && hi > 0);
-        const bool far = !a.table || hi <= -a.b.far || lo >= lut_hi;        // one bias for all of them
-        if (far && !edge && c > 0.0f) {
-            const float beta = !a.table ? 0.0f : (hi <= -a.b.far ? lut[0] : lut[a.b.far + lut_hi]);
+        const bool one = bias.one(lo, hi);
+        const float beta = bias.the_one(hi);
+        if (one && !edge && c > 0.0f) {
             const float base = st.raise(fmaf(largest(s), c, beta)), off = beta - base;
             float sum = 0.0f;
 #pragma unroll
@@ -142,15 +141,28 @@ __global__ __launch_bounds__(256, sizeof(T) * D == 512 ? 1 : 2) void attention_f
             st.l += sum;
         } else {
             const int rel = j0 + 4 * half - i - shift;
+            if (one) {
 #pragma unroll
-            for (int n = 0; n < 2; ++n)
+                for (int n = 0; n < 2; ++n) s[n] = s[n] * c + beta;
+            } else {
 #pragma unroll
-                for (int r = 0; r < 16; ++r) {
-                    const int e = 32 * n + row_of(r, 0);
-                    const float beta = a.table ? lut[distance_index(a.b, rel + e)] : 0.0f;
-                    const bool seen = j0 + 4 * half + e < nk && (!a.causal || rel + e <= 0);
-                    s[n][r] = seen ? fmaf(s[n][r], c, beta) : -INFINITY;
-                }
+                for (int n = 0; n < 2; ++n)
+#pragma unroll
+                    for (int r = 0; r < 16; r += 4) {
+                        const v4f_any t = bias.four(rel + 32 * n + row_of(r, 0));
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) s[n][r + e] = fmaf(s[n][r + e], c, t[e]);
+                    }
+            }
+            if (edge) {
+#pragma unroll
+                for (int n = 0; n < 2; ++n)
+#pragma unroll
+                    for (int r = 0; r < 16; ++r) {
+                        const int e = 32 * n + row_of(r, 0);
+                        if (j0 + 4 * half + e >= nk || (a.causal && rel + e > 0)) s[n][r] = -INFINITY;
+                    }
+            }
             const float base = st.raise(largest(s));
             float sum = 0.0f;
 #pragma unroll
@@ -378,7 +390,7 @@ template <typename T, int D, bool VEC>
 hipError_t go(const AttnArgs &a, hipStream_t st)
 {
     static bool done[kMaxDevices] = {};
-    const size_t lds = 4 * (size_t)kKeyTile * Tile<T, D>::kRowBytes + (a.table ? 4 * (size_t)distance_entries(a.b) : 0);
+    const size_t lds = 4 * (size_t)kKeyTile * Tile<T, D>::kRowBytes + 4 * bias_lut_floats(a);
     const hipError_t e = allow_lds(attention_forward_kernel<T, D, VEC>, lds, done);
     if (e != hipSuccess) return e;
     const int64_t blocks = (int64_t)a.batch * a.heads * ((a.q_len + kRowTile - 1) / kRowTile);
