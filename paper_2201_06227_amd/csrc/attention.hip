@@ -74,9 +74,11 @@ AttnArgs make_args(const egeria_attention_desc *d)
 
 int64_t row_tiles(const egeria_attention_desc *d) { return ((int64_t)d->q_len + kRowTile - 1) / kRowTile; }
 
-// Whether every row of a tensor starts on 16 bytes, holds whole units of 16 and 64 rows span less than 2 GiB.
+// Whether every row of a tensor starts on 16 bytes, holds whole units of 16, rows do not overlap and kRowTile of them span less than
+// 2 GiB.
 bool wide_rows(const egeria_heads *t, const egeria_attention_desc *d)
 {
+    if (t->token_stride < d->head_dim) return false;
     const int64_t size = d->dtype == EGERIA_F32 ? 4 : 2;
     return !((uintptr_t)t->data & 15u) && t->batch_stride * size % 16 == 0 && t->token_stride * size % 16 == 0 && t->head_stride * size % 16 == 0 &&
            d->head_dim * size % 16 == 0 && t->token_stride * size < (0x7fffffffLL - 1024) / kRowTile;

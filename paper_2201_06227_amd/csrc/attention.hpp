@@ -59,6 +59,10 @@ struct v8f {
     float v[8];
 };
 
+template <int N> struct Const {
+    static constexpr int value = N;
+};
+
 __device__ __forceinline__ int clamped(const int32_t *lens, int b, int most)
 {
     const int n = lens ? lens[b] : most;
@@ -135,14 +139,30 @@ struct Tile {
 
     typedef typename FragOf<T>::type frag;
 
-    // rows r0 ... r0 + 31, values 16 kk ... 16 kk + 15
-    static __device__ __forceinline__ frag row_frag(uint32_t lds, int r0, int kk, int lane)
+    // Where a lane reads: what depends on the lane, once; everything else of an address is an exclusive-or or a sum with constants,
+    // since rows 16 apart have the same turn and units are numbered by bits.  (With addresses worked out per read, a step
+    // of the forward kernel for heads of 128 had 41 additions beside 32 reads, and their terms overflowed the registers.)
+    struct Lane {
+        uint32_t row, col;
+    };
+    static __device__ __forceinline__ Lane lane_at(uint32_t lds, int lane)
     {
-        const int r = r0 + (lane & 31), half = lane >> 5;
+        const int half = lane >> 5;
         if constexpr (sizeof(T) == 2) {
-            return __builtin_bit_cast(v8bf, *(const lds_v4u *)(uintptr_t)(lds + at(r, 2 * kk + half)));
+            // across: in each group of 16 lanes, lane i addresses 4 columns of row i / 4 and receives column i of the four rows
+            return {lds + at(lane & 31, half), lds + at(4 * half + ((lane & 15) >> 2), ((lane >> 4) & 1) * 2 + ((lane & 3) >> 1)) + (lane & 1) * 8};
         } else {
-            const v4u lo = *(const lds_v4u *)(uintptr_t)(lds + at(r, 4 * kk + 2 * half)), hi = *(const lds_v4u *)(uintptr_t)(lds + at(r, 4 * kk + 2 * half + 1));
+            return {lds + at(lane & 31, 2 * half), lds + (uint32_t)(4 * half * kRowBytes + ((((lane & 31) >> 2) ^ half) << 4) + (lane & 3) * 4)};
+        }
+    }
+    // rows R0 ... R0 + 31, values 16 kk ... 16 kk + 15 of the tile `off` bytes behind the lane's
+    static __device__ __forceinline__ frag row_frag(const Lane &l, uint32_t off, int r0, int kk)
+    {
+        const uint32_t more = off + (uint32_t)(r0 * kRowBytes);
+        if constexpr (sizeof(T) == 2) {
+            return __builtin_bit_cast(v8bf, *(const lds_v4u *)(uintptr_t)((l.row ^ (uint32_t)(kk << 5)) + more));
+        } else {
+            const v4u lo = *(const lds_v4u *)(uintptr_t)((l.row ^ (uint32_t)(kk << 6)) + more), hi = *(const lds_v4u *)(uintptr_t)((l.row ^ (uint32_t)(kk << 6 | 16)) + more);
             v8f f;
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
@@ -153,22 +173,20 @@ struct Tile {
         }
     }
     // columns 32 db ... 32 db + 31 of the 16 rows from r0 on, in the order of pack()
-    static __device__ __forceinline__ frag col_frag(uint32_t lds, int r0, int db, int lane)
+    static __device__ __forceinline__ frag col_frag(const Lane &l, uint32_t off, int r0, int db)
     {
-        const int half = lane >> 5;
+        const uint32_t more = off + (uint32_t)(r0 * kRowBytes);
         if constexpr (sizeof(T) == 2) {
-            // in each group of 16 lanes, lane i addresses 4 columns of row i / 4 and receives column i of the four rows
-            const int r = r0 + 4 * half + ((lane & 15) >> 2), u = 4 * db + ((lane >> 4) & 1) * 2 + ((lane & 3) >> 1);
-            const v4s lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4s *)(uintptr_t)(lds + at(r, u) + (lane & 1) * 8));
-            const v4s hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4s *)(uintptr_t)(lds + at(r + 8, u) + (lane & 1) * 8));
+            constexpr uint32_t kTurn8 = kUnits == 8 ? 16 : 32;             // turn() of a row 8 further
+            const v4s lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4s *)(uintptr_t)((l.col ^ (uint32_t)(db << 6)) + more));
+            const v4s hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4s *)(uintptr_t)((l.col ^ ((uint32_t)(db << 6) ^ kTurn8)) + more + 8 * kRowBytes));
             return __builtin_bit_cast(v8bf, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
         } else {
-            const int c = 32 * db + (lane & 31);
             v8f f;
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
-                const int r = r0 + 4 * half + (e & 3) + 8 * (e >> 2);
-                f.v[e] = *(const lds_f32 *)(uintptr_t)(lds + at(r, c >> 2) + (c & 3) * 4);
+                const uint32_t unit = (uint32_t)(8 * db) ^ (uint32_t)((e & 3) << 2) ^ (uint32_t)((e >> 2) << 1);
+                f.v[e] = *(const lds_f32 *)(uintptr_t)((l.col ^ (unit << 4)) + more + (uint32_t)(((e & 3) + 8 * (e >> 2)) * kRowBytes));
             }
             return f;
         }
@@ -176,9 +194,9 @@ struct Tile {
 };
 
 // Reads rows of one head of a tensor [.., token, .., feature].
-// VEC: rows start on 16 bytes, hold a whole number of 16-byte units, and 64 of them span less than 2 GiB: buffer loads, straight into
-// LDS.  A unit beyond the row's end or of a token at or beyond `tokens` is asked for beyond the buffer and arrives as zeros.
-// Otherwise: element by element.
+// VEC: rows start on 16 bytes, hold a whole number of 16-byte units, do not overlap, and kRowTile of them span less than 2 GiB:
+// 16-byte loads, into tiles as buffer loads straight into LDS.  A unit beyond the row's end or of a token at or beyond `tokens` is asked
+// for beyond the buffer and arrives as zeros.  Otherwise: element by element.
 template <typename T, int D, bool VEC>
 struct Rows {
     const char *base;
@@ -225,35 +243,51 @@ struct Rows {
             return f;
         }
     }
-    // N tokens from t0 on into a tile, by the THREADS threads numbered tid (whole waves); the requests of the VEC form are
-    // outstanding until an explicit wait
-    template <int N, int THREADS>
-    __device__ __forceinline__ void stage(uint32_t lds, int t0, int tid) const
+};
+
+// Brings N tokens at a time of such rows into tiles, by the THREADS threads numbered tid (whole waves); the requests of the VEC form
+// are outstanding until an explicit wait.  Rows at or beyond `tokens` lie beyond the buffer's extent (rows do not overlap: VEC).
+template <typename T, int D, bool VEC, int N, int THREADS>
+struct Feed {
+    typedef Tile<T, D> tile;
+    static constexpr int kUnits = tile::kUnits, kSteps = N * kUnits / THREADS, kRowsPer = THREADS / kUnits;
+    static_assert(N * kUnits % THREADS == 0, "whole requests");
+    Rows<T, D, VEC> rows;
+    uint32_t off;                           // the lane's place in the first request
+    int tid;
+
+    __device__ __forceinline__ uint32_t place(int i) const
     {
-        typedef Tile<T, D> tile;
-        constexpr int kUnits = tile::kUnits, kSteps = N * kUnits / THREADS;
-        static_assert(N * kUnits % THREADS == 0, "whole requests");
+        const int n = i * THREADS + tid, r = n / kUnits, u = (n % kUnits) ^ tile::turn(r);
+        return u < rows.dim * (int)sizeof(T) / 16 ? (uint32_t)r * (uint32_t)rows.row_bytes + (uint32_t)u * 16u : 0x80000000u;
+    }
+    __device__ __forceinline__ void open(const View &v, int b, int h, int n, int d, int id)
+    {
+        rows.open(v, b, h, n, d);
+        tid = id;
+        if constexpr (VEC) off = place(0);
+    }
+    __device__ __forceinline__ void load(uint32_t lds, int t0) const
+    {
         if constexpr (VEC) {
-            const uint64_t at = (uint64_t)(base + (int64_t)t0 * row_bytes);
+            const uint64_t at = (uint64_t)(rows.base + (int64_t)t0 * rows.row_bytes);
+            const int64_t left = (int64_t)(rows.tokens - t0) * rows.row_bytes;
             v4i rsrc;
             rsrc[0] = __builtin_amdgcn_readfirstlane((int)(uint32_t)at);
             rsrc[1] = __builtin_amdgcn_readfirstlane((int)(uint32_t)(at >> 32) & 0xffff);
-            rsrc[2] = 0x7fffffff;
+            rsrc[2] = __builtin_amdgcn_readfirstlane(left < 0 ? 0 : (left > 0x7fffffff ? 0x7fffffff : (int)left));
             rsrc[3] = kBufferWord;
             const uint32_t first = lds + (uint32_t)__builtin_amdgcn_readfirstlane(tid & ~63) * 16u;
-            const uint32_t step = (uint32_t)row_bytes;
-            const int dim_units = dim * (int)sizeof(T) / 16;
 #pragma unroll
-            for (int i = 0; i < kSteps; ++i) {
-                const int n = i * THREADS + tid, r = n / kUnits, u = (n % kUnits) ^ tile::turn(r);
-                const uint32_t off = t0 + r < tokens && u < dim_units ? (uint32_t)r * step + (uint32_t)u * 16u : 0x80000000u;
-                load_to_lds_b128(rsrc, first + (uint32_t)(i * THREADS * 16), off);
-            }
+            for (int i = 0; i < kSteps; ++i)
+                // rows 16 apart have the same turn: one place, and a multiple of the stride (added to a place outside it stays there)
+                load_to_lds_b128(rsrc, first + (uint32_t)(i * THREADS * 16),
+                                 kRowsPer % 16 == 0 ? off + (uint32_t)(i * kRowsPer) * (uint32_t)rows.row_bytes : place(i));
         } else {
 #pragma unroll
             for (int i = 0; i < kSteps; ++i) {
                 const int n = i * THREADS + tid, r = n / kUnits, u = n % kUnits;
-                *(lds_v4u *)(uintptr_t)(lds + tile::at(r, u)) = unit(t0 + r, u);
+                *(lds_v4u *)(uintptr_t)(lds + tile::at(r, u)) = rows.unit(t0 + r, u);
             }
         }
     }

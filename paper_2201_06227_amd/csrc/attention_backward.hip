@@ -79,16 +79,18 @@ __global__ __launch_bounds__(256, sizeof(T) * D == 512 ? 1 : 2) void attention_d
         for (int i = tid; i < 8 * entries; i += 256) sums[i] = 0.0f;
     float *mine = sums + (2 * wave + half) * entries;
 
-    Rows<T, D, VEC> qr, kr, vr, gr, orow;
+    Rows<T, D, VEC> qr, gr, orow;
     qr.open(a.q, b, h, nq, a.dim);
     gr.open(a.d_o, b, h, nq, a.dim);
     orow.open(a.o, b, h, nq, a.dim);
-    kr.open(a.k, b, h / a.group, nk, a.dim);
-    vr.open(a.v, b, h / a.group, nk, a.dim);
+    Feed<T, D, VEC, kKeys, 256> kr, vr;
+    kr.open(a.k, b, h / a.group, nk, a.dim, tid);
+    vr.open(a.v, b, h / a.group, nk, a.dim, tid);
     if (steps > 0) {
-        kr.template stage<kKeys, 256>(lds, 0, tid);
-        vr.template stage<kKeys, 256>(lds + kTileBytes, 0, tid);
+        kr.load(lds, 0);
+        vr.load(lds + kTileBytes, 0);
     }
+    const typename tile::Lane at = tile::lane_at(lds, lane);
     const int qw = q0 + 32 * wave, i = qw + (lane & 31);
     const int64_t row = ((int64_t)b * a.heads + h) * a.q_len + i;
     typename tile::frag q[D / 16], g[D / 16];
@@ -108,16 +110,16 @@ __global__ __launch_bounds__(256, sizeof(T) * D == 512 ? 1 : 2) void attention_d
     for (int n = 0; n < D / 32; ++n) dq[n] = v16f(0.0f);
     float left = 0.0f, right = 0.0f;                                        // sums of ds beyond the table by distance
 
-    for (int step = 0; step < steps; ++step) {
+    auto one_step = [&](auto buffer, int step) __attribute__((always_inline)) {
+        constexpr uint32_t now = decltype(buffer)::value * 2 * kTileBytes, next = 2 * kTileBytes - now;
         asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
         __syncthreads();
-        const uint32_t now = lds + (step & 1) * 2 * kTileBytes, next = lds + (~step & 1) * 2 * kTileBytes;
         const int j0 = step * kKeys;
         if (step + 1 < steps) {
-            kr.template stage<kKeys, 256>(next, j0 + kKeys, tid);
-            vr.template stage<kKeys, 256>(next + kTileBytes, j0 + kKeys, tid);
+            kr.load(lds + next, j0 + kKeys);
+            vr.load(lds + next + kTileBytes, j0 + kKeys);
         }
-        if (qw >= nq) continue;
+        if (qw >= nq) return;
 #pragma unroll
         for (int n = 0; n < kKeys / 32; ++n) {
             const int jn = j0 + 32 * n;
@@ -125,8 +127,8 @@ __global__ __launch_bounds__(256, sizeof(T) * D == 512 ? 1 : 2) void attention_d
             v16f s = v16f(0.0f), d = v16f(0.0f);
 #pragma unroll
             for (int kk = 0; kk < D / 16; ++kk) {
-                s = mma(tile::row_frag(now, 32 * n, kk, lane), q[kk], s);
-                d = mma(tile::row_frag(now + kTileBytes, 32 * n, kk, lane), g[kk], d);
+                s = mma(tile::row_frag(at, now, 32 * n, kk), q[kk], s);
+                d = mma(tile::row_frag(at, now + kTileBytes, 32 * n, kk), g[kk], d);
             }
             const int lo = jn - (qw + 31) - shift, hi = jn + 31 - qw - shift;             // distances of the wave's pairs
             const bool edge = jn + 32 > nk || (a.causal && hi > 0);
@@ -148,9 +150,10 @@ __global__ __launch_bounds__(256, sizeof(T) * D == 512 ? 1 : 2) void attention_d
 #pragma unroll
             for (int r = 0; r < 16; ++r) s[r] *= d[r] - delta;
             if (edge) {
+const int live = nk - jn - 4 * half, most = a.causal && -rel < live - 1 ? -rel + 1 : live;
 #pragma unroll
                 for (int r = 0; r < 16; ++r)
-                    if (jn + 4 * half + row_of(r, 0) >= nk || (a.causal && rel + row_of(r, 0) > 0)) s[r] = 0.0f;
+                    if (row_of(r, 0) >= most) s[r] = 0.0f;
             }
             if (a.partials) {
                 if (one) {
@@ -165,9 +168,13 @@ __global__ __launch_bounds__(256, sizeof(T) * D == 512 ? 1 : 2) void attention_d
             for (int k = 0; k < 2; ++k) {
                 const typename tile::frag f = pack<T>(s, k);
 #pragma unroll
-                for (int m = 0; m < D / 32; ++m) dq[m] = mma(tile::col_frag(now, 32 * n + 16 * k, m, lane), f, dq[m]);
+                for (int m = 0; m < D / 32; ++m) dq[m] = mma(tile::col_frag(at, now, 32 * n + 16 * k, m), f, dq[m]);
             }
         }
+    };
+    for (int step = 0; step < steps; step += 2) {
+        one_step(Const<0>(), step);
+        if (step + 1 < steps) one_step(Const<1>(), step + 1);
     }
 
     if (i < a.q_len) {
@@ -240,6 +247,7 @@ __global__ __launch_bounds__(256, sizeof(T) * D == 512 ? 1 : 2) void attention_d
     Rows<T, D, VEC> kr, vr;
     kr.open(a.k, b, hk, nk, a.dim);
     vr.open(a.v, b, hk, nk, a.dim);
+    const typename tile::Lane at = tile::lane_at(lds, lane);
     typename tile::frag k[D / 16], v[kValuesInLds ? 1 : D / 16];
     v16f dk[D / 32], dv[D / 32];
 #pragma unroll
@@ -247,14 +255,16 @@ __global__ __launch_bounds__(256, sizeof(T) * D == 512 ? 1 : 2) void attention_d
 
     // stages the queries of a step: rows into LDS, statistics into registers (the caller stores them once the step before is done)
     float next_base = 0.0f, next_delta = 0.0f;
-    auto stage = [&](int step) {
+    Feed<T, D, VEC, kQueries, 256> qr, gr;
+    qr.open(a.q, b, 0, nq, a.dim, tid);
+    gr.open(a.d_o, b, 0, nq, a.dim, tid);
+    const char *q_base = qr.rows.base, *g_base = gr.rows.base;
+    auto stage = [&](uint32_t to, int step) __attribute__((always_inline)) {
         const int h = hk * a.group + step / per_head, i0 = first + step % per_head * kQueries;
-        const uint32_t to = lds + (step & 1) * 2 * kTileBytes;
-        Rows<T, D, VEC> qr, gr;
-        qr.open(a.q, b, h, nq, a.dim);
-        gr.open(a.d_o, b, h, nq, a.dim);
-        qr.template stage<kQueries, 256>(to, i0, tid);
-        gr.template stage<kQueries, 256>(to + kTileBytes, i0, tid);
+        qr.rows.base = q_base + (int64_t)h * a.q.sh * (int64_t)sizeof(T);
+        gr.rows.base = g_base + (int64_t)h * a.d_o.sh * (int64_t)sizeof(T);
+        qr.load(to, i0);
+        gr.load(to + kTileBytes, i0);
         if (tid < kQueries) {
             const int i = i0 + tid < nq ? i0 + tid : nq - 1;
             const int64_t row = ((int64_t)b * a.heads + h) * a.q_len + i;
@@ -270,8 +280,12 @@ __global__ __launch_bounds__(256, sizeof(T) * D == 512 ? 1 : 2) void attention_d
         }
     };
     if (steps > 0) {
-        if constexpr (kValuesInLds) vr.template stage<kRowTile, 256>(lds + 4 * kTileBytes, k0, tid);
-        stage(0);
+        if constexpr (kValuesInLds) {
+            Feed<T, D, VEC, kRowTile, 256> values;
+            values.open(a.v, b, hk, nk, a.dim, tid);
+            values.load(lds + 4 * kTileBytes, k0);
+        }
+        stage(lds, 0);
         keep(0);
 #pragma unroll
         for (int kk = 0; kk < D / 16; ++kk) {
@@ -280,7 +294,10 @@ __global__ __launch_bounds__(256, sizeof(T) * D == 512 ? 1 : 2) void attention_d
         }
     }
     int lut_head = -1;
-    for (int step = 0; step < steps; ++step) {
+    const typename tile::Lane at_v = tile::lane_at(lds + 4 * kTileBytes + 32 * wave * tile::kRowBytes, lane);
+    auto one_step = [&](auto buffer, int step) __attribute__((always_inline)) {
+        constexpr int kBuffer = decltype(buffer)::value;
+        constexpr uint32_t now = kBuffer * 2 * kTileBytes, next = 2 * kTileBytes - now;
         const int h = hk * a.group + step / per_head, i0 = first + step % per_head * kQueries;
         asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
         __syncthreads();
@@ -289,8 +306,7 @@ __global__ __launch_bounds__(256, sizeof(T) * D == 512 ? 1 : 2) void attention_d
             lut_head = h;
             __syncthreads();
         }
-        const uint32_t now = lds + (step & 1) * 2 * kTileBytes;
-        if (step + 1 < steps) stage(step + 1);
+        if (step + 1 < steps) stage(lds + next, step + 1);
 #pragma unroll
         for (int n = 0; n < kQueries / 32; ++n) {
             const int in = i0 + 32 * n;
@@ -298,10 +314,10 @@ __global__ __launch_bounds__(256, sizeof(T) * D == 512 ? 1 : 2) void attention_d
             v16f s = v16f(0.0f), d = v16f(0.0f);
 #pragma unroll
             for (int kk = 0; kk < D / 16; ++kk) {
-                s = mma(tile::row_frag(now, 32 * n, kk, lane), k[kk], s);
+                s = mma(tile::row_frag(at, now, 32 * n, kk), k[kk], s);
                 if constexpr (kValuesInLds)
-                    d = mma(tile::row_frag(now + kTileBytes, 32 * n, kk, lane), tile::row_frag(lds + 4 * kTileBytes, 32 * wave, kk, lane), d);
-                else d = mma(tile::row_frag(now + kTileBytes, 32 * n, kk, lane), v[kk], d);
+                    d = mma(tile::row_frag(at, now + kTileBytes, 32 * n, kk), tile::row_frag(at_v, 0, 0, kk), d);
+                else d = mma(tile::row_frag(at, now + kTileBytes, 32 * n, kk), v[kk], d);
             }
             const int lo = jw - (in + 31) - shift, hi = jw + 31 - in - shift;             // distances of the wave's pairs
             const bool one = bias.one(lo, hi);
@@ -310,7 +326,7 @@ __global__ __launch_bounds__(256, sizeof(T) * D == 512 ? 1 : 2) void attention_d
             v16f p;
 #pragma unroll
             for (int r = 0; r < 16; r += 4) {
-                const float4 base = *(const float4 *)&stat[step & 1][0][32 * n + row_of(r, half)];
+                const float4 base = *(const float4 *)&stat[kBuffer][0][32 * n + row_of(r, half)];
                 const float bs[4] = {base.x, base.y, base.z, base.w};
                 v4f_any t;
                 if (one) t = v4f_any(beta);
@@ -325,7 +341,7 @@ __global__ __launch_bounds__(256, sizeof(T) * D == 512 ? 1 : 2) void attention_d
             }
 #pragma unroll
             for (int r = 0; r < 16; r += 4) {
-                const float4 delta = *(const float4 *)&stat[step & 1][1][32 * n + row_of(r, half)];
+                const float4 delta = *(const float4 *)&stat[kBuffer][1][32 * n + row_of(r, half)];
                 const float ds[4] = {delta.x, delta.y, delta.z, delta.w};
 #pragma unroll
                 for (int e = 0; e < 4; ++e) s[r + e] = p[r + e] * (d[r + e] - ds[e]);
@@ -335,12 +351,16 @@ __global__ __launch_bounds__(256, sizeof(T) * D == 512 ? 1 : 2) void attention_d
                 const typename tile::frag fp = pack<T>(p, e), fs = pack<T>(s, e);
 #pragma unroll
                 for (int m = 0; m < D / 32; ++m) {
-                    dv[m] = mma(tile::col_frag(now + kTileBytes, 32 * n + 16 * e, m, lane), fp, dv[m]);
-                    dk[m] = mma(tile::col_frag(now, 32 * n + 16 * e, m, lane), fs, dk[m]);
+                    dv[m] = mma(tile::col_frag(at, now + kTileBytes, 32 * n + 16 * e, m), fp, dv[m]);
+                    dk[m] = mma(tile::col_frag(at, now, 32 * n + 16 * e, m), fs, dk[m]);
                 }
             }
         }
         if (step + 1 < steps) keep(step + 1);
+    };
+    for (int step = 0; step < steps; step += 2) {
+        one_step(Const<0>(), step);
+        if (step + 1 < steps) one_step(Const<1>(), step + 1);
     }
 
     if (j < a.k_len) {

@@ -28,31 +28,37 @@ struct RowState {
     }
     // S^T of N blocks of 32 keys
     template <int N>
-    __device__ __forceinline__ void scores(v16f (&s)[N], uint32_t k_lds, int lane) const
+    __device__ __forceinline__ void scores(v16f (&s)[N], const typename tile::Lane &at, uint32_t k_off) const
     {
 #pragma unroll
         for (int n = 0; n < N; ++n) s[n] = v16f(0.0f);
 #pragma unroll
         for (int kk = 0; kk < kDepth; ++kk)
 #pragma unroll
-            for (int n = 0; n < N; ++n) s[n] = mma(tile::row_frag(k_lds, 32 * n, kk, lane), q[kk], s[n]);
+            for (int n = 0; n < N; ++n) s[n] = mma(tile::row_frag(at, k_off, 32 * n, kk), q[kk], s[n]);
     }
-    // what is summed so far moves to the maximum `top` (both lanes of a query agree on it)
+    // The reference that exponents are taken against after a step with maximum `top` (both lanes of a query agree on it).  It follows
+    // the maximum only when that has grown by more than kSlack: until then p <= 2^kSlack, which costs neither fp32 sums nor bf16
+    // operands precision, and what is summed so far need not be rescaled.  (Following it always, some query of a wave has a
+    // new maximum in most steps: SLACK_MEASURE.)
+    static constexpr float kSlack = 8.0f;
     __device__ __forceinline__ float raise(float top)
     {
         top = fmaxf(top, lane_xor<32>(top));
-        const float to = fmaxf(m, top), base = to == -INFINITY ? 0.0f : to;
-        if (__any(to > m)) {
-            const float keep = __builtin_amdgcn_exp2f(m - base);
+        if (__any(top > m + kSlack || (m == -INFINITY && top > m))) {
+            asm volatile("" ::: "memory");                                 // a branch, not 64 speculated products
+            const float to = fmaxf(m, top), keep = __builtin_amdgcn_exp2f(m - (to == -INFINITY ? 0.0f : to));
             l *= keep;
 #pragma unroll
-            for (int i = 0; i < kBlocks; ++i) o[i] *= keep;
+            for (int i = 0; i < kBlocks; ++i)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) o[i][r] *= keep;
+            m = to;
         }
-        m = to;
-        return base;
+        return m == -INFINITY ? 0.0f : m;
     }
     template <int N>
-    __device__ __forceinline__ void add(const v16f (&p)[N], uint32_t v_lds, int lane)
+    __device__ __forceinline__ void add(const v16f (&p)[N], const typename tile::Lane &at, uint32_t v_off)
     {
 #pragma unroll
         for (int n = 0; n < N; ++n)
@@ -60,7 +66,7 @@ struct RowState {
             for (int s = 0; s < 2; ++s) {
                 const typename tile::frag f = pack<T>(p[n], s);
 #pragma unroll
-                for (int i = 0; i < kBlocks; ++i) o[i] = mma(tile::col_frag(v_lds, 32 * n + 16 * s, i, lane), f, o[i]);
+                for (int i = 0; i < kBlocks; ++i) o[i] = mma(tile::col_frag(at, v_off, 32 * n + 16 * s, i), f, o[i]);
             }
     }
 };
@@ -97,14 +103,16 @@ __global__ __launch_bounds__(256, sizeof(T) * D == 512 ? 1 : 2) void attention_f
     bias.open(a, (float *)(smem + 4 * kTileBytes));
     bias.fill(a, h, tid);
 
-    Rows<T, D, VEC> qr, kr, vr;
+    Rows<T, D, VEC> qr;
     qr.open(a.q, b, h, nq, a.dim);
-    kr.open(a.k, b, h / a.group, nk, a.dim);
-    vr.open(a.v, b, h / a.group, nk, a.dim);
+    Feed<T, D, VEC, kKeyTile, 256> kr, vr;
+    kr.open(a.k, b, h / a.group, nk, a.dim, tid);
+    vr.open(a.v, b, h / a.group, nk, a.dim, tid);
     if (steps > 0) {
-        kr.template stage<kKeyTile, 256>(lds, 0, tid);
-        vr.template stage<kKeyTile, 256>(lds + kTileBytes, 0, tid);
+        kr.load(lds, 0);
+        vr.load(lds + kTileBytes, 0);
     }
+    const typename tile::Lane at = tile::lane_at(lds, lane);
     const int qw = q0 + 32 * wave, i = qw + (lane & 31);
     RowState<T, D> st;
     st.clear();
@@ -112,69 +120,61 @@ __global__ __launch_bounds__(256, sizeof(T) * D == 512 ? 1 : 2) void attention_f
     for (int kk = 0; kk < D / 16; ++kk) st.q[kk] = qr.frag(qw, kk, lane);
     const float c = a.scale * kLog2e;
 
-    for (int step = 0; step < steps; ++step) {
+    auto one_step = [&](auto buffer, int step) __attribute__((always_inline)) {
+        constexpr uint32_t now = decltype(buffer)::value * 2 * kTileBytes, next = 2 * kTileBytes - now;
         asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
         __syncthreads();                                                    // this step's tiles are there, the other pair is free
-        const uint32_t now = lds + (step & 1) * 2 * kTileBytes, next = lds + (~step & 1) * 2 * kTileBytes;
         const int j0 = step * kKeyTile;
         if (step + 1 < steps) {
-            kr.template stage<kKeyTile, 256>(next, j0 + kKeyTile, tid);
-            vr.template stage<kKeyTile, 256>(next + kTileBytes, j0 + kKeyTile, tid);
+            kr.load(lds + next, j0 + kKeyTile);
+            vr.load(lds + next + kTileBytes, j0 + kKeyTile);
         }
-        if (qw >= nq || (a.causal && j0 > qw + 31 + shift)) continue;       // no pair of the wave is visible
+        if (qw >= nq || (a.causal && j0 > qw + 31 + shift)) return;         // no pair of the wave is visible
         v16f s[2];
-        st.scores(s, now, lane);
+        st.scores(s, at, now);
         const int lo = j0 - (qw + 31) - shift, hi = j0 + kKeyTile - 1 - qw - shift;       // distances of the wave's pairs
         const bool edge = j0 + kKeyTile > nk || (a.causal && hi > 0);
         const bool one = bias.one(lo, hi);
-        const float beta = bias.the_one(hi);
-        if (one && !edge && c > 0.0f) {
-            const float base = st.raise(fmaf(largest(s), c, beta)), off = beta - base;
-            float sum = 0.0f;
-#pragma unroll
-            for (int n = 0; n < 2; ++n)
-#pragma unroll
-                for (int r = 0; r < 16; ++r) {
-                    s[n][r] = __builtin_amdgcn_exp2f(fmaf(s[n][r], c, off));
-                    sum += s[n][r];
-                }
-            st.l += sum;
-        } else {
+        // scores times `by` plus `beta`, unless they have to be worked out pair by pair (both ways end in the same code: as two of
+        // their own the compiler copied the whole sum to and fro)
+        float by = c, beta = bias.the_one(hi);
+        if (!one || edge || !(c > 0.0f)) {
             const int rel = j0 + 4 * half - i - shift;
-            if (one) {
-#pragma unroll
-                for (int n = 0; n < 2; ++n) s[n] = s[n] * c + beta;
-            } else {
-#pragma unroll
-                for (int n = 0; n < 2; ++n)
-#pragma unroll
-                    for (int r = 0; r < 16; r += 4) {
-                        const v4f_any t = bias.four(rel + 32 * n + row_of(r, 0));
-#pragma unroll
-                        for (int e = 0; e < 4; ++e) s[n][r + e] = fmaf(s[n][r + e], c, t[e]);
-                    }
-            }
-            if (edge) {
-#pragma unroll
-                for (int n = 0; n < 2; ++n)
-#pragma unroll
-                    for (int r = 0; r < 16; ++r) {
-                        const int e = 32 * n + row_of(r, 0);
-                        if (j0 + 4 * half + e >= nk || (a.causal && rel + e > 0)) s[n][r] = -INFINITY;
-                    }
-            }
-            const float base = st.raise(largest(s));
-            float sum = 0.0f;
 #pragma unroll
             for (int n = 0; n < 2; ++n)
 #pragma unroll
-                for (int r = 0; r < 16; ++r) {
-                    s[n][r] = __builtin_amdgcn_exp2f(s[n][r] - base);
-                    sum += s[n][r];
+                for (int r = 0; r < 16; r += 4) {
+                    v4f_any t = v4f_any(beta);
+                    if (!one) t = bias.four(rel + 32 * n + row_of(r, 0));
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) s[n][r + e] = fmaf(s[n][r + e], c, t[e]);
                 }
-            st.l += sum;
+            if (edge) {
+                const int live = nk - j0 - 4 * half, most = a.causal && -rel < live - 1 ? -rel + 1 : live;
+#pragma unroll
+                for (int n = 0; n < 2; ++n)
+#pragma unroll
+                    for (int r = 0; r < 16; ++r)
+                        if (32 * n + row_of(r, 0) >= most) s[n][r] = -INFINITY;
+            }
+            by = 1.0f;
+            beta = 0.0f;
         }
-        st.add(s, now + kTileBytes, lane);
+        const float off = beta - st.raise(fmaf(largest(s), by, beta));
+        float sum = 0.0f;
+#pragma unroll
+        for (int n = 0; n < 2; ++n)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) {
+                s[n][r] = __builtin_amdgcn_exp2f(fmaf(s[n][r], by, off));
+                sum += s[n][r];
+            }
+        st.l += sum;
+        st.add(s, at, now + kTileBytes);
+    };
+    for (int step = 0; step < steps; step += 2) {
+        one_step(Const<0>(), step);
+        if (step + 1 < steps) one_step(Const<1>(), step + 1);
     }
 
     const float total = st.l + lane_xor<32>(st.l);
@@ -250,25 +250,23 @@ __global__ __launch_bounds__(256) void attention_few_kernel(AttnArgs a)
     }
     const float c = a.scale * kLog2e;
     const float *my_tab = tab + (hl - h0) * a.table_rows;
-    Rows<T, D, VEC> kr, vr;
-    kr.open(a.k, b, g, nk, a.dim);
-    vr.open(a.v, b, g, nk, a.dim);
+    Feed<T, D, VEC, kFewKeys, 64> kr, vr;
+    kr.open(a.k, b, g, nk, a.dim, lane);
+    vr.open(a.v, b, g, nk, a.dim, lane);
+    const typename Tile<T, D>::Lane at_lane = Tile<T, D>::lane_at(lds, lane);
     if (a.table) __syncthreads();
     constexpr int kLoads = 2 * kFewKeys * Tile<T, D>::kUnits / 64;         // requests of one step
     int j0 = k0 + kFewKeys * wave;
     auto stage = [&](uint32_t to, int j) {
         asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");                 // the buffer has been read
-        kr.template stage<kFewKeys, 64>(to, j, lane);
-        vr.template stage<kFewKeys, 64>(to + L::kTileBytes, j, lane);
+        kr.load(lds + to, j);
+        vr.load(lds + to + L::kTileBytes, j);
     };
-    uint32_t buf = 0;
-    if (L::kBuffers == 2 && j0 < k1) stage(lds, j0);
-    for (; j0 < k1; j0 += 4 * kFewKeys) {
-        const uint32_t now = lds + buf * 2 * L::kTileBytes;
+    auto one_step = [&](auto buffer, int j0) __attribute__((always_inline)) {
+        constexpr uint32_t now = decltype(buffer)::value * 2 * L::kTileBytes, next = 2 * L::kTileBytes - now;
         if (L::kBuffers == 2) {
-            buf ^= 1u;
             if (j0 + 4 * kFewKeys < k1) {
-                stage(lds + buf * 2 * L::kTileBytes, j0 + 4 * kFewKeys);
+                stage(next, j0 + 4 * kFewKeys);
                 if (VEC) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(kLoads) : "memory");
             } else asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
         } else {
@@ -277,7 +275,7 @@ __global__ __launch_bounds__(256) void attention_few_kernel(AttnArgs a)
         }
         wave_lds_turn();
         v16f s[1];
-        st.scores(s, now, lane);
+        st.scores(s, at_lane, now);
         const int rel = j0 - i - shift;                                     // distances rel ... rel + 31
         const bool edge = j0 + kFewKeys > nk || (a.causal && __any(rel + kFewKeys - 1 > 0));
         float beta = 0.0f;
@@ -302,7 +300,15 @@ __global__ __launch_bounds__(256) void attention_few_kernel(AttnArgs a)
             sum += s[0][e];
         }
         st.l += sum;
-        st.add(s, now + L::kTileBytes, lane);
+        st.add(s, at_lane, now + L::kTileBytes);
+    };
+    if (L::kBuffers == 2 && j0 < k1) stage(0, j0);
+    for (; j0 < k1; j0 += 4 * kFewKeys) {
+        one_step(Const<0>(), j0);
+        if (L::kBuffers == 2) {
+            j0 += 4 * kFewKeys;
+            if (j0 < k1) one_step(Const<1>(), j0);
+        }
     }
     __syncthreads();                                                        // every wave is done with its tiles
     st.l += lane_xor<32>(st.l);
