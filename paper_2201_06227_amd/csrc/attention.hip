@@ -105,9 +105,19 @@ int few_splits(const egeria_attention_desc *d)
     return n < 1 ? 1 : (int)n;
 }
 
+// Parts that the steps of a backward kernel's workgroups are dealt in where there are few of them, each a sum in fp32 that a last
+// launch adds up: enough for `want` workgroups, of two steps at least, at most 16.
+int parts_of(int64_t blocks, int64_t steps, int64_t want)
+{
+    if (blocks == 0 || blocks * 2 > want) return 1;
+    int64_t n = (want + blocks - 1) / blocks;
+    n = n > steps / 2 ? steps / 2 : n;
+    return n < 1 ? 1 : (n > 16 ? 16 : (int)n);
+}
+
 struct Plan {
-    size_t off_delta = 0, off_part = 0, off_o = 0, off_ml = 0, total = 0;
-    int splits = 0;
+    size_t off_delta = 0, off_part = 0, off_o = 0, off_ml = 0, off_q = 0, off_kv = 0, total = 0;
+    int splits = 0, q_parts = 1, kv_parts = 1;
 };
 Plan make_plan(const egeria_attention_desc *d, bool backward)
 {
@@ -116,7 +126,12 @@ Plan make_plan(const egeria_attention_desc *d, bool backward)
     take(256);
     if (backward) {
         p.off_delta = take((size_t)d->batch * d->heads * d->q_len * 4);
-        p.off_part = take((size_t)d->batch * d->heads * row_tiles(d) * position_rows(d->bias) * 4);
+        const int64_t key_tiles = ((int64_t)d->k_len + kRowTile - 1) / kRowTile, wide = d->head_dim <= 64 ? 64 : 128;
+        p.q_parts = parts_of((int64_t)d->batch * d->heads * row_tiles(d), key_tiles * kRowTile / kKeyTile, 512);
+        p.kv_parts = parts_of((int64_t)d->batch * d->kv_heads * key_tiles, row_tiles(d) * kRowTile / kKeyTile * (d->heads / d->kv_heads), 1024);
+        p.off_part = take((size_t)d->batch * d->heads * row_tiles(d) * p.q_parts * position_rows(d->bias) * 4);
+        if (p.q_parts > 1) p.off_q = take((size_t)p.q_parts * d->batch * d->heads * d->q_len * wide * 4);
+        if (p.kv_parts > 1) p.off_kv = take((size_t)p.kv_parts * d->batch * d->kv_heads * d->k_len * wide * 8);
         return p;
     }
     p.splits = few_splits(d);
@@ -200,11 +215,13 @@ egeria_status egeria_attention_backward(const egeria_attention_desc *desc, const
     a.lse = const_cast<float *>(lse);
     a.delta = (float *)((char *)ws + p.off_delta);
     a.partials = dtable ? (float *)((char *)ws + p.off_part) : nullptr;
+    a.dtable = dtable;
+    a.q_parts = p.q_parts, a.kv_parts = p.kv_parts;
+    a.part_q = (float *)((char *)ws + p.off_q), a.part_kv = (float *)((char *)ws + p.off_kv);
     hipStream_t st = (hipStream_t)stream;
     bool vec = true;
     for (const egeria_heads *t : {dout, q, k, v, out, dq, dk, dv}) vec = vec && wide_rows(t, desc);
     EG_HIP(launch_attention_backward(a, (egeria_dtype)desc->dtype, vec, st));
-    if (dtable) EG_HIP(launch_table_reduce(a.partials, a.heads, (int64_t)a.batch * row_tiles(desc), a.table_rows, dtable, st));
     return EGERIA_OK;
 }
 

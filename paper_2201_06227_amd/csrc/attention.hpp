@@ -13,13 +13,15 @@ struct AttnArgs {
     View q, k, v, o, d_o, dq, dk, dv;
     float *lse;                             // [batch, heads, q_len]
     float *delta;                           // [batch, heads, q_len], backward
-    float *partials;                        // [heads][batch * row tiles][buckets], backward with a table gradient
+    float *partials;                        // [heads][batch * parts * row tiles][buckets], backward with a table gradient
+    float *dtable;                          // [buckets, heads] out, or null
     float *split_o, *split_ml;              // forward split over keys: partial outputs and row statistics
+    float *part_q, *part_kv;                // backward in parts: [parts][batch, heads, q_len][D], [parts][batch, kv_heads, k_len][dk, dv][D]
     const int32_t *q_lens, *k_lens;
     const float *table;                     // null: no bias
     int32_t table_rows;
     int32_t batch, heads, kv_heads, group, q_len, k_len, dim, causal;
-    int32_t splits;
+    int32_t splits, q_parts, kv_parts;
     float scale;
     Buckets b;
 };
@@ -33,7 +35,7 @@ hipError_t launch_attention_forward(const AttnArgs &a, egeria_dtype dt, bool vec
 // few rows: a.splits workgroups share a row tile's keys; more than one leaves partial results (split_o, split_ml) that a second
 // launch joins
 hipError_t launch_attention_few(const AttnArgs &a, egeria_dtype dt, bool vec, hipStream_t st);
-// dq, delta and the partial sums of the table's gradient; then dk and dv
+// dq, delta and the partial sums of the table's gradient; then dk, dv and the table's gradient; then, in parts, their sums
 hipError_t launch_attention_backward(const AttnArgs &a, egeria_dtype dt, bool vec, hipStream_t st);
 
 // a launcher's instance for the type, the head size and how the rows are read

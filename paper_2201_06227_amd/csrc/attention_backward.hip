@@ -62,12 +62,14 @@ __global__ __launch_bounds__(256, sizeof(T) * D == 512 ? 1 : 2) void attention_d
     const int tid = threadIdx.x, lane = tid & 63, half = lane >> 5, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const uint32_t tiles = (uint32_t)(a.q_len + kRowTile - 1) / kRowTile, piece = xcd_piece(blockIdx.x, gridDim.x);
     const uint32_t rt = tiles - 1 - piece % tiles;                          // the longest rows of a causal head first
-    const int q0 = (int)rt * kRowTile, h = (int)(piece / tiles % (uint32_t)a.heads), b = (int)(piece / tiles / (uint32_t)a.heads);
+    const int part = (int)(piece / tiles % (uint32_t)a.q_parts), bh = (int)(piece / tiles / (uint32_t)a.q_parts);
+    const int q0 = (int)rt * kRowTile, h = bh % a.heads, b = bh / a.heads;
     const int nq = clamped(a.q_lens, b, a.q_len), nk = clamped(a.k_lens, b, a.k_len), shift = a.causal ? nk - nq : 0;
     const int rows = nq - q0 < kRowTile ? nq - q0 : kRowTile;
     int keys = rows > 0 ? nk : 0;
     if (a.causal && keys > q0 + rows + shift) keys = q0 + rows + shift;
-    const int steps = keys > 0 ? (keys + kKeys - 1) / kKeys : 0;
+    const int all = keys > 0 ? (keys + kKeys - 1) / kKeys : 0;
+    const int begin = (int)((int64_t)all * part / a.q_parts), steps = (int)((int64_t)all * (part + 1) / a.q_parts);
 
     const uint32_t lds = (uint32_t)(uintptr_t)(lds_byte *)smem;
     BiasLut bias;
@@ -86,9 +88,9 @@ __global__ __launch_bounds__(256, sizeof(T) * D == 512 ? 1 : 2) void attention_d
     Feed<T, D, VEC, kKeys, 256> kr, vr;
     kr.open(a.k, b, h / a.group, nk, a.dim, tid);
     vr.open(a.v, b, h / a.group, nk, a.dim, tid);
-    if (steps > 0) {
-        kr.load(lds, 0);
-        vr.load(lds + kTileBytes, 0);
+    if (begin < steps) {
+        kr.load(lds, begin * kKeys);
+        vr.load(lds + kTileBytes, begin * kKeys);
     }
     const typename tile::Lane at = tile::lane_at(lds, lane);
     const int qw = q0 + 32 * wave, i = qw + (lane & 31);
@@ -102,7 +104,7 @@ __global__ __launch_bounds__(256, sizeof(T) * D == 512 ? 1 : 2) void attention_d
         delta += dot(g[kk], orow.frag(qw, kk, lane));
     }
     delta += lane_xor<32>(delta);
-    if (half == 0 && i < a.q_len) a.delta[row] = delta;
+    if (half == 0 && i < a.q_len && part == 0) a.delta[row] = delta;
     const float lse = i < nq ? a.lse[row] : -INFINITY;
     const float base = lse == -INFINITY ? INFINITY : lse * kLog2e, c = a.scale * kLog2e;
     v16f dq[D / 32];
@@ -172,44 +174,34 @@ const int live = nk - jn - 4 * half, most = a.causal && -rel < live - 1 ? -rel +
             }
         }
     };
-    for (int step = 0; step < steps; step += 2) {
+    for (int step = begin; step < steps; step += 2) {
         one_step(Const<0>(), step);
         if (step + 1 < steps) one_step(Const<1>(), step + 1);
     }
 
     if (i < a.q_len) {
         T *out = (T *)a.dq.p + ((int64_t)b * a.dq.sb + (int64_t)i * a.dq.st + (int64_t)h * a.dq.sh);
-        const float k = i < nq ? a.scale : 0.0f;
+        float *sum = a.part_q + (((int64_t)part * a.batch * a.heads + bh) * a.q_len + i) * D;
 #pragma unroll
         for (int n = 0; n < D / 32; ++n)
 #pragma unroll
-            for (int r = 0; r < 16; r += 4)
-                store4<T, VEC>(out, 32 * n + row_of(r, half), a.dim, dq[n][r] * k, dq[n][r + 1] * k, dq[n][r + 2] * k, dq[n][r + 3] * k);
+            for (int r = 0; r < 16; r += 4) {
+                const int f = 32 * n + row_of(r, half);
+                float x[4];
+#pragma unroll
+                for (int e = 0; e < 4; ++e) x[e] = i < nq ? dq[n][r + e] * a.scale : 0.0f;
+                if (a.q_parts > 1) *(float4 *)(sum + f) = make_float4(x[0], x[1], x[2], x[3]);
+                else store4<T, VEC>(out, f, a.dim, x[0], x[1], x[2], x[3]);
+            }
     }
     if (a.partials) {
         left = wave_sum(left);
         right = wave_sum(right);
-        __syncthreads();
-        if (lane == 0) {
+        if (lane == 0) {                                                   // the wave's own table: in order after its additions
             mine[0] += left;
             mine[entries - 1] += right;
         }
-        __syncthreads();
-        // a bucket for each group of four lanes
-        for (int n = tid >> 2; n < a.table_rows; n += 64) {
-            int count, at = entries_of_bucket(a.b, n, &count);
-            // the table's ends have the same buckets as the distances beyond them
-            if (count > 0 && at + count == entries - 2 * kPad) count += kPad;
-            if (count > 0 && at == 0) count += kPad;
-            else at += kPad;
-            float s = 0.0f;
-            for (int e = tid & 3; e < count; e += 4)
-#pragma unroll
-                for (int w = 0; w < 8; ++w) s += sums[w * entries + at + e];
-            s += lane_xor<1>(s);
-            s += lane_xor<2>(s);
-            if ((tid & 3) == 0) a.partials[(((int64_t)h * a.batch + b) * tiles + rt) * a.table_rows + n] = s;
-        }
+        bucket_sums(a.b, sums, 8, entries, kPad, a.table_rows, a.partials + (((int64_t)h * a.batch + b) * a.q_parts * tiles + part * tiles + rt) * a.table_rows);
     }
 }
 
@@ -230,13 +222,22 @@ __global__ __launch_bounds__(256, sizeof(T) * D == 512 ? 1 : 2) void attention_d
     constexpr bool kValuesInLds = D > 64;
     __shared__ float stat[2][2][kQueries];                                  // base-2 log-sum-exp and delta of a step's queries
     const int tid = threadIdx.x, lane = tid & 63, half = lane >> 5, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const uint32_t tiles = (uint32_t)(a.k_len + kRowTile - 1) / kRowTile, piece = xcd_piece(blockIdx.x, gridDim.x);
-    const int k0 = (int)(piece % tiles) * kRowTile, hk = (int)(piece / tiles % (uint32_t)a.kv_heads), b = (int)(piece / tiles / (uint32_t)a.kv_heads);
+    // the table's gradient, whose partial sums the dq kernel has left: the first workgroups
+    const uint32_t extra = a.dtable ? (uint32_t)a.heads : 0u;
+    if (blockIdx.x < extra) {
+        const int64_t row_tiles = (a.q_len + kRowTile - 1) / kRowTile;
+        reduce_table(a.partials, a.heads, (int64_t)a.batch * a.q_parts * row_tiles, a.table_rows, a.dtable, (int)blockIdx.x, (double *)smem);
+        return;
+    }
+    const uint32_t tiles = (uint32_t)(a.k_len + kRowTile - 1) / kRowTile, piece = xcd_piece(blockIdx.x - extra, gridDim.x - extra);
+    const int part = (int)(piece / tiles % (uint32_t)a.kv_parts), bh = (int)(piece / tiles / (uint32_t)a.kv_parts);
+    const int k0 = (int)(piece % tiles) * kRowTile, hk = bh % a.kv_heads, b = bh / a.kv_heads;
     const int nq = clamped(a.q_lens, b, a.q_len), nk = clamped(a.k_lens, b, a.k_len), shift = a.causal ? nk - nq : 0;
     // queries that see a key of the tile: from `first` on; the same for every head of the group
     int first = a.causal && k0 > shift ? (k0 - shift) / kQueries * kQueries : 0;
     const int per_head = k0 < nk && first < nq ? (nq - first + kQueries - 1) / kQueries : 0;
-    const int steps = per_head * a.group;
+    const int64_t all = (int64_t)per_head * a.group;
+    const int begin = (int)(all * part / a.kv_parts), steps = (int)(all * (part + 1) / a.kv_parts);
 
     const uint32_t lds = (uint32_t)(uintptr_t)(lds_byte *)smem;
     constexpr int kStage = 4 * kTileBytes + (kValuesInLds ? kRowTile * tile::kRowBytes : 0);
@@ -273,19 +274,19 @@ __global__ __launch_bounds__(256, sizeof(T) * D == 512 ? 1 : 2) void attention_d
             if (i0 + tid >= nq) next_base = -INFINITY;
         }
     };
-    auto keep = [&](int step) {
+    auto keep = [&](int buffer) {
         if (tid < kQueries) {
-            stat[step & 1][0][tid] = next_base == -INFINITY ? INFINITY : next_base * kLog2e;
-            stat[step & 1][1][tid] = next_delta;
+            stat[buffer][0][tid] = next_base == -INFINITY ? INFINITY : next_base * kLog2e;
+            stat[buffer][1][tid] = next_delta;
         }
     };
-    if (steps > 0) {
+    if (begin < steps) {
         if constexpr (kValuesInLds) {
             Feed<T, D, VEC, kRowTile, 256> values;
             values.open(a.v, b, hk, nk, a.dim, tid);
             values.load(lds + 4 * kTileBytes, k0);
         }
-        stage(lds, 0);
+        stage(lds, begin);
         keep(0);
 #pragma unroll
         for (int kk = 0; kk < D / 16; ++kk) {
@@ -356,9 +357,9 @@ __global__ __launch_bounds__(256, sizeof(T) * D == 512 ? 1 : 2) void attention_d
                 }
             }
         }
-        if (step + 1 < steps) keep(step + 1);
+        if (step + 1 < steps) keep(1 - kBuffer);
     };
-    for (int step = 0; step < steps; step += 2) {
+    for (int step = begin; step < steps; step += 2) {
         one_step(Const<0>(), step);
         if (step + 1 < steps) one_step(Const<1>(), step + 1);
     }
@@ -367,6 +368,7 @@ __global__ __launch_bounds__(256, sizeof(T) * D == 512 ? 1 : 2) void attention_d
         T *ok = (T *)a.dk.p + ((int64_t)b * a.dk.sb + (int64_t)j * a.dk.st + (int64_t)hk * a.dk.sh);
         T *ov = (T *)a.dv.p + ((int64_t)b * a.dv.sb + (int64_t)j * a.dv.st + (int64_t)hk * a.dv.sh);
         const bool live = j < nk;
+        float *sum = a.part_kv + (((int64_t)part * a.batch * a.kv_heads + bh) * a.k_len + j) * (2 * D);
 #pragma unroll
         for (int n = 0; n < D / 32; ++n)
 #pragma unroll
@@ -378,10 +380,43 @@ __global__ __launch_bounds__(256, sizeof(T) * D == 512 ? 1 : 2) void attention_d
                     x[e] = live ? dk[n][r + e] * a.scale : 0.0f;
                     y[e] = live ? dv[n][r + e] : 0.0f;
                 }
-                store4<T, VEC>(ok, f, a.dim, x[0], x[1], x[2], x[3]);
-                store4<T, VEC>(ov, f, a.dim, y[0], y[1], y[2], y[3]);
+                if (a.kv_parts > 1) {
+                    *(float4 *)(sum + f) = make_float4(x[0], x[1], x[2], x[3]);
+                    *(float4 *)(sum + D + f) = make_float4(y[0], y[1], y[2], y[3]);
+                } else {
+                    store4<T, VEC>(ok, f, a.dim, x[0], x[1], x[2], x[3]);
+                    store4<T, VEC>(ov, f, a.dim, y[0], y[1], y[2], y[3]);
+                }
             }
     }
+}
+
+// Joins parts of sums: one of up to three tensors [batch, heads, len, D] in each blockIdx.y, a thread for four features of a row.
+struct JoinJob {
+    View out;
+    const float *sum;                       // [parts][batch * heads * len][stride]
+    int64_t rows;
+    int32_t heads, len, parts, stride;
+};
+struct JoinJobs {
+    JoinJob job[3];
+};
+template <typename T, int D, bool VEC>
+__global__ __launch_bounds__(256) void attention_join_parts_kernel(JoinJobs jobs, int dim)
+{
+    const JoinJob &j = jobs.job[blockIdx.y];
+    constexpr int kPer = 256 / (D / 4);
+    const int f = threadIdx.x % (D / 4) * 4;
+    const int64_t row = (int64_t)blockIdx.x * kPer + threadIdx.x / (D / 4);
+    if (row >= j.rows) return;
+    float4 s = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+    for (int p = 0; p < j.parts; ++p) {
+        const float4 x = *(const float4 *)(j.sum + ((int64_t)p * j.rows + row) * j.stride + f);
+        s.x += x.x, s.y += x.y, s.z += x.z, s.w += x.w;
+    }
+    const int i = (int)(row % j.len), h = (int)(row / j.len % j.heads), b = (int)(row / j.len / j.heads);
+    T *out = (T *)j.out.p + ((int64_t)b * j.out.sb + (int64_t)i * j.out.st + (int64_t)h * j.out.sh);
+    store4<T, VEC>(out, f, dim, s.x, s.y, s.z, s.w);
 }
 
 template <typename T, int D, bool VEC>
@@ -389,24 +424,38 @@ hipError_t go_backward(const AttnArgs &a, hipStream_t st)
 {
     static bool done_q[kMaxDevices] = {}, done_kv[kMaxDevices] = {};
     const size_t row = (size_t)Tile<T, D>::kRowBytes, lut = bias_lut_floats(a);
-    if (a.batch == 0) return hipSuccess;
-    if (a.q_len > 0) {
+    const int64_t q_blocks = (int64_t)a.batch * a.heads * ((a.q_len + kRowTile - 1) / kRowTile) * a.q_parts;
+    const int64_t k_blocks = (int64_t)a.batch * a.kv_heads * ((a.k_len + kRowTile - 1) / kRowTile) * a.kv_parts + (a.dtable ? a.heads : 0);
+    if (q_blocks > 0) {
         const size_t lds = 4 * dq_keys<T, D>() * row + 4 * lut * (a.partials ? 9 : 1);
         hipError_t e = allow_lds(attention_dq_kernel<T, D, VEC>, lds, done_q);
         if (e != hipSuccess) return e;
-        const int64_t blocks = (int64_t)a.batch * a.heads * ((a.q_len + kRowTile - 1) / kRowTile);
-        e = launch_k(EGERIA_KERNEL_ATTENTION, attention_dq_kernel<T, D, VEC>, dim3((unsigned)blocks), dim3(256), lds, st, a);
+        e = launch_k(EGERIA_KERNEL_ATTENTION, attention_dq_kernel<T, D, VEC>, dim3((unsigned)q_blocks), dim3(256), lds, st, a);
         if (e != hipSuccess) return e;
     }
-    if (a.k_len > 0) {
+    if (k_blocks > 0) {
         const size_t lds = 4 * dkv_queries<D>() * row + (D > 64 ? kRowTile * row : 0) + 4 * lut;
         hipError_t e = allow_lds(attention_dkv_kernel<T, D, VEC>, lds, done_kv);
         if (e != hipSuccess) return e;
-        const int64_t blocks = (int64_t)a.batch * a.kv_heads * ((a.k_len + kRowTile - 1) / kRowTile);
-        e = launch_k(EGERIA_KERNEL_ATTENTION, attention_dkv_kernel<T, D, VEC>, dim3((unsigned)blocks), dim3(256), lds, st, a);
+        e = launch_k(EGERIA_KERNEL_ATTENTION, attention_dkv_kernel<T, D, VEC>, dim3((unsigned)k_blocks), dim3(256), lds, st, a);
         if (e != hipSuccess) return e;
     }
-    return hipSuccess;
+    JoinJobs jobs = {};
+    int n = 0;
+    int64_t most = 0;
+    auto join = [&](const View &out, const float *sum, int heads, int len, int parts, int stride) {
+        const int64_t rows = (int64_t)a.batch * heads * len;
+        if (parts < 2 || rows == 0) return;
+        jobs.job[n++] = {out, sum, rows, heads, len, parts, stride};
+        most = rows > most ? rows : most;
+    };
+    join(a.dq, a.part_q, a.heads, a.q_len, a.q_parts, D);
+    join(a.dk, a.part_kv, a.kv_heads, a.k_len, a.kv_parts, 2 * D);
+    join(a.dv, a.part_kv + D, a.kv_heads, a.k_len, a.kv_parts, 2 * D);
+    if (n == 0) return hipSuccess;
+    const int64_t per = 256 / (D / 4);
+    return launch_k(EGERIA_KERNEL_NONE, attention_join_parts_kernel<T, D, VEC>, dim3((unsigned)((most + per - 1) / per), (unsigned)n), dim3(256), 0, st,
+                    jobs, (int)a.dim);
 }
 
 }  // namespace

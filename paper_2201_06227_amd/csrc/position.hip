@@ -167,28 +167,8 @@ __global__ __launch_bounds__(256) void position_bias_backward_kernel(Buckets b, 
 __global__ __launch_bounds__(256) void table_reduce_kernel(const float *__restrict__ partials, int heads, int64_t parts, int buckets,
                                                            float *__restrict__ dtable)
 {
-    __shared__ double sm[256];
-    const int h = blockIdx.x;
-    // groups of `width` threads (a power of two, one for each bucket) take the parts in turn
-    int width = 1;
-    while (width < buckets) width <<= 1;
-    const int groups = 256 / width, g = threadIdx.x / width, n = threadIdx.x % width;
-    double s = 0.0;
-    if (n < buckets) {
-        const float *src = partials + (int64_t)h * parts * buckets + n;
-        int64_t i = g;
-        for (; i + 3 * groups < parts; i += 4 * groups) {
-            const float a = src[i * buckets], c = src[(i + groups) * buckets], d = src[(i + 2 * groups) * buckets], f = src[(i + 3 * groups) * buckets];
-            s += ((double)a + (double)c) + ((double)d + (double)f);
-        }
-        for (; i < parts; i += groups) s += (double)src[i * buckets];
-    }
-    sm[threadIdx.x] = s;
-    __syncthreads();
-    if (g == 0 && n < buckets) {
-        for (int k = 1; k < groups; ++k) s += sm[k * width + n];
-        dtable[n * heads + h] = (float)s;
-    }
+    __shared__ double memory[256];
+    reduce_table(partials, heads, parts, buckets, dtable, blockIdx.x, memory);
 }
 
 // How the gradient's rows, columns and batch are dealt to workgroups: eight rows each where that is few workgroups, more where
@@ -224,12 +204,12 @@ bool valid_sizes(const egeria_position_table *t, int32_t heads, int32_t q_len, i
 
 int64_t parts_of(const Pieces &p) { return (int64_t)p.shares * p.row_blocks * p.col_blocks; }
 
-}  // namespace
-
 hipError_t launch_table_reduce(const float *partials, int heads, int64_t parts, int buckets, float *dtable, hipStream_t st)
 {
     return launch_k(EGERIA_KERNEL_NONE, table_reduce_kernel, dim3((unsigned)heads), dim3(256), 0, st, partials, heads, parts, buckets, dtable);
 }
+
+}  // namespace
 
 }  // namespace egeria
 

@@ -81,9 +81,62 @@ __device__ __forceinline__ int entries_of_bucket(const Buckets &b, int row, int 
     *count = hi > lo ? hi - lo : 0;
     return right ? b.far + lo : b.far - hi + 1;
 }
-#endif
 
-// dtable [buckets, heads] of the partial sums [heads][parts][buckets], summed in this order in fp64
-hipError_t launch_table_reduce(const float *partials, int heads, int64_t parts, int buckets, float *dtable, hipStream_t st);
+// What a workgroup of 256 threads makes of sums by distance: copies [copies][stride] in LDS, of entries -far - pad ... hi + pad each, to
+// the sums by bucket out[0 .. rows).  Distances beyond the table's ends belong to the ends' buckets.
+__device__ __forceinline__ void bucket_sums(const Buckets &b, float *sums, int copies, int stride, int pad, int rows, float *out)
+{
+    const int entries = b.far + (b.both ? b.far : 0) + 1, tid = threadIdx.x, lane = tid & 63;
+    __syncthreads();
+    for (int e = tid; e < entries + 2 * pad; e += 256) {
+        float s = sums[e];
+        for (int w = 1; w < copies; ++w) s += sums[w * stride + e];
+        sums[e] = s;
+    }
+    __syncthreads();
+    for (int n = tid >> 6; n < rows; n += 4) {
+        int count, at = entries_of_bucket(b, n, &count);
+        if (count > 0) {
+            if (at + count == entries) count += pad;
+            if (at == 0) count += pad;
+            else at += pad;
+        }
+        float s = 0.0f;
+        for (int e = lane; e < count; e += 64) s += sums[at + e];
+        s = wave_sum(s);
+        if (lane == 0) out[n] = s;
+    }
+}
+
+// dtable [buckets, heads], head h, of the partial sums [heads][parts][buckets], in this order and in fp64, by a workgroup of 256 threads;
+// memory: 2 KiB of LDS
+__device__ __forceinline__ void reduce_table(const float *__restrict__ partials, int heads, int64_t parts, int buckets, float *__restrict__ dtable,
+                                             int h, double *memory)
+{
+    // groups of `width` threads (a power of two, one for each bucket) take the parts in turn
+    int width = 1;
+    while (width < buckets) width <<= 1;
+    const int groups = 256 / width, g = threadIdx.x / width, n = threadIdx.x % width;
+    double s = 0.0;
+    if (n < buckets) {
+        const float *src = partials + (int64_t)h * parts * buckets + n;
+        int64_t i = g;
+        for (; i + 7 * groups < parts; i += 8 * groups) {
+            float x[8];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) x[e] = src[(i + e * groups) * buckets];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) s += (double)x[e];
+        }
+        for (; i < parts; i += groups) s += (double)src[i * buckets];
+    }
+    memory[threadIdx.x] = s;
+    __syncthreads();
+    if (g == 0 && n < buckets) {
+        for (int k = 1; k < groups; ++k) s += memory[k * width + n];
+        dtable[n * heads + h] = (float)s;
+    }
+}
+#endif
 
 }  // namespace egeria
