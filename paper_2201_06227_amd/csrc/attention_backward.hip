@@ -226,7 +226,7 @@ __global__ __launch_bounds__(256, sizeof(T) * D == 512 ? 1 : 2) void attention_d
     const uint32_t extra = a.dtable ? (uint32_t)a.heads : 0u;
     if (blockIdx.x < extra) {
         const int64_t row_tiles = (a.q_len + kRowTile - 1) / kRowTile;
-        reduce_table(a.partials, a.heads, (int64_t)a.batch * a.q_parts * row_tiles, a.table_rows, a.dtable, (int)blockIdx.x, (double *)smem);
+        reduce_table<256>(a.partials, a.heads, (int64_t)a.batch * a.q_parts * row_tiles, a.table_rows, a.dtable, (int)blockIdx.x, (double *)smem);
         return;
     }
     const uint32_t tiles = (uint32_t)(a.k_len + kRowTile - 1) / kRowTile, piece = xcd_piece(blockIdx.x - extra, gridDim.x - extra);

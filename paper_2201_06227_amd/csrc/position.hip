@@ -33,24 +33,29 @@ template <> __device__ __forceinline__ uint16_t narrow<uint16_t>(float v)
     return __builtin_bit_cast(uint16_t, (__bf16)v);
 }
 
-// One workgroup: `rows` rows (a multiple of kRows) of one head, 256 units of 16 bytes of their columns.
+// Where a thread's patches lie: 2^lg units of 16 bytes side by side (32 to 256 of them, so that half a wave has one row of patches),
+// 256 / 2^lg patches below each other, `rows` rows to a workgroup.
+struct Deal {
+    int lg, rows;
+    uint32_t row_blocks, col_blocks, shares;
+};
+
 template <typename T>
 __global__ __launch_bounds__(256) void position_bias_kernel(Buckets b, const float *__restrict__ table, int heads, int q_len, int k_len,
-                                                            int offset, int rows, uint32_t row_blocks, uint32_t col_blocks,
-                                                            T *__restrict__ out)
+                                                            int offset, Deal deal, T *__restrict__ out)
 {
     constexpr int N = Unit<T>::N;
     typedef typename Unit<T>::vec vec;
     extern __shared__ float lut[];
     const uint32_t p = xcd_piece(blockIdx.x, gridDim.x);
-    const uint32_t cb = p % col_blocks, rb = p / col_blocks % row_blocks, h = p / col_blocks / row_blocks;
+    const uint32_t cb = p % deal.col_blocks, rb = p / deal.col_blocks % deal.row_blocks, h = p / deal.col_blocks / deal.row_blocks;
     const int entries = b.both ? 2 * b.far + 1 : b.far + 1;
     for (int i = threadIdx.x; i < entries; i += 256) lut[spread(i)] = table[bucket_of_entry(b, i) * heads + h];
     __syncthreads();
-    const int j0 = (int)(cb * 256 + threadIdx.x) * N;
+    const int j0 = (int)((cb << deal.lg) + (threadIdx.x & ((1 << deal.lg) - 1))) * N;
     if (j0 >= k_len) return;
-    const int last = (int)rb * rows + rows < q_len ? (int)rb * rows + rows : q_len;
-    for (int i0 = rb * rows; i0 < last; i0 += kRows) {
+    const int last = (int)rb * deal.rows + deal.rows < q_len ? (int)rb * deal.rows + deal.rows : q_len;
+    for (int i0 = (int)rb * deal.rows + (int)(threadIdx.x >> deal.lg) * kRows; i0 < last; i0 += kRows << (8 - deal.lg)) {
         T v[kRows + N - 1];                                        // distances first, first + 1, ...
         const int first = j0 - (i0 + kRows - 1) - offset;
 #pragma unroll
@@ -74,30 +79,29 @@ __global__ __launch_bounds__(256) void position_bias_kernel(Buckets b, const flo
 }
 
 // One workgroup: the same piece of the rows and columns, summed over its share of the batch.  A thread adds up its patch along the
-// diagonals in registers, over the batch, then the diagonals' sums go to a table by distance of its wave in LDS.  The lanes of a
-// wave add to different entries at each step and a wave's additions are in order: the result does not depend on timing.
+// diagonals in registers, over the batch, then the diagonals' sums go to a table by distance of its half wave in LDS.  The lanes of
+// half a wave add to different entries at each step and a wave's additions are in order: the result does not depend on timing.
 template <typename T>
 __global__ __launch_bounds__(256) void position_bias_backward_kernel(Buckets b, const T *__restrict__ dbias, int64_t batch, int heads,
-                                                                     int q_len, int k_len, int offset, int rows, uint32_t row_blocks,
-                                                                     uint32_t col_blocks, uint32_t shares, int rows_of_table,
+                                                                     int q_len, int k_len, int offset, Deal deal, int rows_of_table,
                                                                      float *__restrict__ partials)
 {
     constexpr int N = Unit<T>::N;
     typedef typename Unit<T>::vec vec;
-    extern __shared__ float sums[];                                // [4 waves][stride]
+    extern __shared__ float sums[];                                // [8 half waves][entries]
     const uint32_t p = xcd_piece(blockIdx.x, gridDim.x);
-    const uint32_t cb = p % col_blocks, rb = p / col_blocks % row_blocks, sh = p / col_blocks / row_blocks % shares;
-    const uint32_t h = p / col_blocks / row_blocks / shares;
-    const int entries = b.both ? 2 * b.far + 1 : b.far + 1, stride = spread(entries - 1) + 1;
-    for (int i = threadIdx.x; i < 4 * stride; i += 256) sums[i] = 0.0f;
+    const uint32_t cb = p % deal.col_blocks, rb = p / deal.col_blocks % deal.row_blocks, sh = p / deal.col_blocks / deal.row_blocks % deal.shares;
+    const uint32_t h = p / deal.col_blocks / deal.row_blocks / deal.shares;
+    const int entries = b.both ? 2 * b.far + 1 : b.far + 1;
+    for (int i = threadIdx.x; i < 8 * entries; i += 256) sums[i] = 0.0f;
     __syncthreads();
-    float *mine = sums + (threadIdx.x >> 6) * stride;
-    const int64_t b0 = batch * sh / shares, b1 = batch * (sh + 1) / shares;
-    const int j0 = (int)(cb * 256 + threadIdx.x) * N;
-    const int last = (int)rb * rows + rows < q_len ? (int)rb * rows + rows : q_len;
+    float *mine = sums + (threadIdx.x >> 5) * entries;
+    const int64_t b0 = batch * sh / deal.shares, b1 = batch * (sh + 1) / deal.shares;
+    const int j0 = (int)((cb << deal.lg) + (threadIdx.x & ((1 << deal.lg) - 1))) * N;
+    const int last = (int)rb * deal.rows + deal.rows < q_len ? (int)rb * deal.rows + deal.rows : q_len;
     float left = 0.0f, right = 0.0f;                               // patches whose distances all lie beyond the table
     const int hi = b.both ? b.far : 0;
-    for (int i0 = rb * rows; i0 < last; i0 += kRows) {
+    for (int i0 = (int)rb * deal.rows + (int)(threadIdx.x >> deal.lg) * kRows; i0 < last; i0 += kRows << (8 - deal.lg)) {
         float d[kRows + N - 1];
 #pragma unroll
         for (int e = 0; e < kRows + N - 1; ++e) d[e] = 0.0f;
@@ -133,58 +137,45 @@ __global__ __launch_bounds__(256) void position_bias_backward_kernel(Buckets b, 
 #pragma unroll
             for (int e = 0; e < kRows + N - 1; ++e) {
                 const int rel = first + e;
-                // entries inside the table are different in every lane; what lies beyond its ends is the lane's own sum
+                // entries inside the table are different in every lane of the half; what lies beyond its ends is the lane's own sum
                 if (rel <= -b.far) left += d[e];
                 else if (rel >= hi) right += d[e];
-                else __hip_atomic_fetch_add(&mine[spread(rel + b.far)], d[e], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
+                else mine[rel + b.far] += d[e];
             }
         }
     }
     left = wave_sum(left);
     right = wave_sum(right);
-    __syncthreads();
+    wave_lds_turn();
     if ((threadIdx.x & 63) == 0) {
         mine[0] += left;                                           // the ends of the table have the same buckets as what lies beyond
-        mine[spread(entries - 1)] += right;
+        mine[entries - 1] += right;
     }
-    __syncthreads();
-    // a bucket for each group of four lanes
-    const int64_t part = ((int64_t)sh * row_blocks + rb) * col_blocks + cb, parts = (int64_t)shares * row_blocks * col_blocks;
-    for (int n = threadIdx.x >> 2; n < rows_of_table; n += 64) {
-        int count;
-        const int at = entries_of_bucket(b, n, &count);
-        float s = 0.0f;
-        for (int i = threadIdx.x & 3; i < count; i += 4) {
-            const int w = spread(at + i);
-            s += (sums[w] + sums[w + stride]) + (sums[w + 2 * stride] + sums[w + 3 * stride]);
-        }
-        s += lane_xor<1>(s);
-        s += lane_xor<2>(s);
-        if ((threadIdx.x & 3) == 0) partials[((int64_t)h * parts + part) * rows_of_table + n] = s;
-    }
+    const int64_t part = ((int64_t)sh * deal.row_blocks + rb) * deal.col_blocks + cb, parts = (int64_t)deal.shares * deal.row_blocks * deal.col_blocks;
+    bucket_sums(b, sums, 8, entries, 0, rows_of_table, partials + ((int64_t)h * parts + part) * rows_of_table);
 }
 
-__global__ __launch_bounds__(256) void table_reduce_kernel(const float *__restrict__ partials, int heads, int64_t parts, int buckets,
+constexpr int kReduceThreads = 1024;
+__global__ __launch_bounds__(kReduceThreads) void table_reduce_kernel(const float *__restrict__ partials, int heads, int64_t parts, int buckets,
                                                            float *__restrict__ dtable)
 {
-    __shared__ double memory[256];
-    reduce_table(partials, heads, parts, buckets, dtable, blockIdx.x, memory);
+    __shared__ double memory[kReduceThreads];
+    reduce_table<kReduceThreads>(partials, heads, parts, buckets, dtable, blockIdx.x, memory);
 }
 
-// How the gradient's rows, columns and batch are dealt to workgroups: eight rows each where that is few workgroups, more where
-// that still leaves 2048, and the batch in shares where rows and columns alone do not give 1024.
-struct Pieces {
-    int rows;
-    uint32_t row_blocks, col_blocks, shares;
-};
-Pieces make_pieces(int64_t batch, int heads, int q_len, int k_len, int per_unit, bool split_batch)
+// How rows, columns and, for the gradient, the batch are dealt to workgroups: one patch for each thread, more rows where that still
+// leaves 2048 workgroups, and the batch in shares where rows and columns alone do not give 1024.
+Deal make_deal(int64_t batch, int heads, int q_len, int k_len, int per_unit, bool split_batch)
 {
-    Pieces p;
-    p.col_blocks = (uint32_t)(((int64_t)k_len + 256 * per_unit - 1) / (256 * per_unit));
-    p.rows = kRows;
-    auto blocks = [&](int rows) { return (int64_t)((q_len + (int64_t)rows - 1) / rows) * p.col_blocks * heads; };
-    while (p.rows < 64 && blocks(2 * p.rows) >= 2048) p.rows *= 2;
-    p.row_blocks = (uint32_t)((q_len + (int64_t)p.rows - 1) / p.rows);
+    Deal p;
+    const int64_t units = ((int64_t)k_len + per_unit - 1) / per_unit;
+    p.lg = 5;
+    while (p.lg < 8 && (1 << p.lg) < units) ++p.lg;
+    p.col_blocks = (uint32_t)((units + (1 << p.lg) - 1) >> p.lg);
+    p.rows = kRows << (8 - p.lg);
+    auto blocks = [&](int rows) { return ((int64_t)q_len + rows - 1) / rows * p.col_blocks * heads; };
+    for (int n = 0; n < 3 && blocks(2 * p.rows) >= 2048; ++n) p.rows *= 2;
+    p.row_blocks = (uint32_t)(((int64_t)q_len + p.rows - 1) / p.rows);
     int64_t shares = 1;
     if (split_batch) {
         shares = blocks(p.rows) > 0 ? (1024 + blocks(p.rows) - 1) / blocks(p.rows) : 1;
@@ -202,11 +193,11 @@ bool valid_sizes(const egeria_position_table *t, int32_t heads, int32_t q_len, i
     return offset >= -(1 << 29) && offset <= (1 << 29) && q_len <= (1 << 29) && k_len <= (1 << 29);
 }
 
-int64_t parts_of(const Pieces &p) { return (int64_t)p.shares * p.row_blocks * p.col_blocks; }
+int64_t parts_of(const Deal &p) { return (int64_t)p.shares * p.row_blocks * p.col_blocks; }
 
 hipError_t launch_table_reduce(const float *partials, int heads, int64_t parts, int buckets, float *dtable, hipStream_t st)
 {
-    return launch_k(EGERIA_KERNEL_NONE, table_reduce_kernel, dim3((unsigned)heads), dim3(256), 0, st, partials, heads, parts, buckets, dtable);
+    return launch_k(EGERIA_KERNEL_NONE, table_reduce_kernel, dim3((unsigned)heads), dim3(kReduceThreads), 0, st, partials, heads, parts, buckets, dtable);
 }
 
 }  // namespace
@@ -224,14 +215,14 @@ egeria_status egeria_position_bias(const egeria_position_table *t, int32_t heads
     if (q_len == 0 || k_len == 0) return EGERIA_OK;
     if (!bias || ((uintptr_t)bias & 15u)) return EGERIA_ERR_INVALID_ARG;
     const Buckets b = make_buckets(t);
-    const Pieces p = make_pieces(1, heads, q_len, k_len, dt == EGERIA_F32 ? 4 : 8, false);
+    const Deal p = make_deal(1, heads, q_len, k_len, dt == EGERIA_F32 ? 4 : 8, false);
     const int64_t blocks = parts_of(p) * heads;
     if (blocks > 0x7fffffffLL) return EGERIA_ERR_UNSUPPORTED;
     const int entries = distance_entries(b);
     const size_t lds = 4 * (size_t)(entries + entries / 64 + 1);
     auto go = [&](auto kernel, auto *out) {
         return launch_k(EGERIA_KERNEL_NONE, kernel, dim3((unsigned)blocks), dim3(256), lds, (hipStream_t)stream, b, t->table, (int)heads,
-                        (int)q_len, (int)k_len, (int)offset, p.rows, p.row_blocks, p.col_blocks, out);
+                        (int)q_len, (int)k_len, (int)offset, p, out);
     };
     const hipError_t e = dt == EGERIA_F32 ? go(position_bias_kernel<float>, (float *)bias) : go(position_bias_kernel<uint16_t>, (uint16_t *)bias);
     return e == hipSuccess ? EGERIA_OK : EGERIA_ERR_HIP;
@@ -241,7 +232,7 @@ size_t egeria_position_bias_workspace_bytes(const egeria_position_table *t, int3
                                             egeria_dtype dt)
 {
     if (!valid_sizes(t, heads, q_len, k_len, 0, dt) || batch < 0) return 0;
-    const Pieces p = make_pieces(batch, heads, q_len, k_len, dt == EGERIA_F32 ? 4 : 8, true);
+    const Deal p = make_deal(batch, heads, q_len, k_len, dt == EGERIA_F32 ? 4 : 8, true);
     return align_up((size_t)parts_of(p) * heads * t->buckets * 4, 256) + 256;
 }
 
@@ -258,14 +249,13 @@ egeria_status egeria_position_bias_backward(const egeria_position_table *t, cons
     float *partials = (float *)ws;
     if (none) return launch_table_reduce(partials, heads, 0, t->buckets, dtable, st) == hipSuccess ? EGERIA_OK : EGERIA_ERR_HIP;
     const Buckets b = make_buckets(t);
-    const Pieces p = make_pieces(batch, heads, q_len, k_len, dt == EGERIA_F32 ? 4 : 8, true);
+    const Deal p = make_deal(batch, heads, q_len, k_len, dt == EGERIA_F32 ? 4 : 8, true);
     const int64_t blocks = parts_of(p) * heads;
     if (blocks > 0x7fffffffLL) return EGERIA_ERR_UNSUPPORTED;
-    const int entries = distance_entries(b);
-    const size_t lds = 16 * (size_t)(entries + entries / 64 + 1);
+    const size_t lds = 32 * (size_t)distance_entries(b);
     auto go = [&](auto kernel, auto *src) {
         return launch_k(EGERIA_KERNEL_NONE, kernel, dim3((unsigned)blocks), dim3(256), lds, st, b, src, (int64_t)batch, (int)heads, (int)q_len,
-                        (int)k_len, (int)offset, p.rows, p.row_blocks, p.col_blocks, p.shares, (int)t->buckets, partials);
+                        (int)k_len, (int)offset, p, (int)t->buckets, partials);
     };
     hipError_t e = dt == EGERIA_F32 ? go(position_bias_backward_kernel<float>, (const float *)dbias)
                                     : go(position_bias_backward_kernel<uint16_t>, (const uint16_t *)dbias);

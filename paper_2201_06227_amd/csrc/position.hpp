@@ -108,27 +108,26 @@ __device__ __forceinline__ void bucket_sums(const Buckets &b, float *sums, int c
     }
 }
 
-// dtable [buckets, heads], head h, of the partial sums [heads][parts][buckets], in this order and in fp64, by a workgroup of 256 threads;
-// memory: 2 KiB of LDS
+// dtable [buckets, heads], head h, of the partial sums [heads][parts][buckets], in this order and in fp64, by a workgroup of THREADS;
+// memory: one double for each
+template <int THREADS>
 __device__ __forceinline__ void reduce_table(const float *__restrict__ partials, int heads, int64_t parts, int buckets, float *__restrict__ dtable,
                                              int h, double *memory)
 {
     // groups of `width` threads (a power of two, one for each bucket) take the parts in turn
     int width = 1;
     while (width < buckets) width <<= 1;
-    const int groups = 256 / width, g = threadIdx.x / width, n = threadIdx.x % width;
+    const int groups = THREADS / width, g = threadIdx.x / width, n = threadIdx.x % width;
     double s = 0.0;
     if (n < buckets) {
         const float *src = partials + (int64_t)h * parts * buckets + n;
-        int64_t i = g;
-        for (; i + 7 * groups < parts; i += 8 * groups) {
-            float x[8];
+        for (int64_t i = g; i < parts; i += 8 * groups) {
+            float x[8];                                                    // eight loads in flight
 #pragma unroll
-            for (int e = 0; e < 8; ++e) x[e] = src[(i + e * groups) * buckets];
+            for (int e = 0; e < 8; ++e) x[e] = src[(i + e * groups < parts ? i + e * groups : i) * buckets];
 #pragma unroll
-            for (int e = 0; e < 8; ++e) s += (double)x[e];
+            for (int e = 0; e < 8; ++e) s += i + e * groups < parts ? (double)x[e] : 0.0;
         }
-        for (; i < parts; i += groups) s += (double)src[i * buckets];
     }
     memory[threadIdx.x] = s;
     __syncthreads();
