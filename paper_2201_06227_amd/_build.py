@@ -8,7 +8,8 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libegeria.so")
 SOURCES = ["api.hip", "quantize.hip", "gemm_i8.hip", "gram.hip", "bert.hip", "freeze.hip", "cache.hip", "cast.hip", "affine.hip", "microbench.hip",
-           "attention.hip", "attention_forward.hip", "attention_backward.hip", "position.hip"]
+           "attention.hip", "attention_forward.hip", "attention_backward.hip",
+           "attention_one_pass.hip", "position.hip"]
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 
 FLAGS = [
@@ -30,7 +31,7 @@ def sources():
 def headers():
     include = os.path.join(os.path.dirname(HERE), "include")
     return ([os.path.join(include, h) for h in ("egeria.h", "egeria_profile.h")] +
-            [os.path.join(CSRC, h) for h in ("common.hpp", "position.hpp", "attention.hpp", "gelu.hpp", "gelu_table.inc", "gelu_lines.inc")])
+            [os.path.join(CSRC, h) for h in ("common.hpp", "position.hpp", "attention.hpp", "attention_diagonals.hpp", "gelu.hpp", "gelu_table.inc", "gelu_lines.inc")])
 
 
 def is_stale() -> bool:

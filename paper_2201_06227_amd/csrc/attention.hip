@@ -74,14 +74,14 @@ AttnArgs make_args(const egeria_attention_desc *d)
 
 int64_t row_tiles(const egeria_attention_desc *d) { return ((int64_t)d->q_len + kRowTile - 1) / kRowTile; }
 
-// Whether every row of a tensor starts on 16 bytes, holds whole units of 16, rows do not overlap and kRowTile of them span less than
-// 2 GiB.
+// Whether every row of a tensor starts on 16 bytes, holds whole units of 16, rows do not overlap and as many as a tile
+// has at most span less than 2 GiB.
 bool wide_rows(const egeria_heads *t, const egeria_attention_desc *d)
 {
     if (t->token_stride < d->head_dim) return false;
     const int64_t size = d->dtype == EGERIA_F32 ? 4 : 2;
     return !((uintptr_t)t->data & 15u) && t->batch_stride * size % 16 == 0 && t->token_stride * size % 16 == 0 && t->head_stride * size % 16 == 0 &&
-           d->head_dim * size % 16 == 0 && t->token_stride * size < (0x7fffffffLL - 1024) / kRowTile;
+           d->head_dim * size % 16 == 0 && t->token_stride * size < (0x7fffffffLL - 1024) / (kOnePassKeys > kRowTile ? kOnePassKeys : kRowTile);
 }
 
 int64_t few_tiles(const egeria_attention_desc *d)
@@ -115,7 +115,15 @@ int parts_of(int64_t blocks, int64_t steps, int64_t want)
     return n < 1 ? 1 : (n > 16 ? 16 : (int)n);
 }
 
+// The backward kernel that makes everything in one pass: where its keys and LDS fit and a workgroup for each key head of the batch
+// gives half the compute units work.
+bool one_pass(const egeria_attention_desc *d)
+{
+    return d->k_len <= kOnePassKeys && d->head_dim <= 64 && (int64_t)d->batch * d->kv_heads >= 128 && one_pass_lds(d, true) <= kMostLds;
+}
+
 struct Plan {
+    bool one = false;
     size_t off_delta = 0, off_part = 0, off_o = 0, off_ml = 0, off_q = 0, off_kv = 0, total = 0;
     int splits = 0, q_parts = 1, kv_parts = 1;
 };
@@ -124,6 +132,11 @@ Plan make_plan(const egeria_attention_desc *d, bool backward)
     Plan p;
     auto take = [&](size_t bytes) { size_t o = p.total; p.total += align_up(bytes, 256); return o; };
     take(256);
+    if (backward && one_pass(d)) {
+        p.one = true;
+        p.off_part = take((size_t)d->batch * d->heads * position_rows(d->bias) * 4);
+        return p;
+    }
     if (backward) {
         p.off_delta = take((size_t)d->batch * d->heads * d->q_len * 4);
         const int64_t key_tiles = ((int64_t)d->k_len + kRowTile - 1) / kRowTile, wide = d->head_dim <= 64 ? 64 : 128;
@@ -221,7 +234,8 @@ egeria_status egeria_attention_backward(const egeria_attention_desc *desc, const
     hipStream_t st = (hipStream_t)stream;
     bool vec = true;
     for (const egeria_heads *t : {dout, q, k, v, out, dq, dk, dv}) vec = vec && wide_rows(t, desc);
-    EG_HIP(launch_attention_backward(a, (egeria_dtype)desc->dtype, vec, st));
+    a.table_parts = (int64_t)a.batch * (p.one ? 1 : a.q_parts * row_tiles(desc));
+    EG_HIP((p.one ? launch_attention_one_pass : launch_attention_backward)(a, (egeria_dtype)desc->dtype, vec, st));
     return EGERIA_OK;
 }
 

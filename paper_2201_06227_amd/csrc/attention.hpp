@@ -22,6 +22,7 @@ struct AttnArgs {
     int32_t table_rows;
     int32_t batch, heads, kv_heads, group, q_len, k_len, dim, causal;
     int32_t splits, q_parts, kv_parts;
+    int64_t table_parts;                    // partial sums of each head in `partials`
     float scale;
     Buckets b;
 };
@@ -37,6 +38,11 @@ hipError_t launch_attention_forward(const AttnArgs &a, egeria_dtype dt, bool vec
 hipError_t launch_attention_few(const AttnArgs &a, egeria_dtype dt, bool vec, hipStream_t st);
 // dq, delta and the partial sums of the table's gradient; then dk, dv and the table's gradient; then, in parts, their sums
 hipError_t launch_attention_backward(const AttnArgs &a, egeria_dtype dt, bool vec, hipStream_t st);
+// everything in one pass, for at most kOnePassKeys keys and heads of at most 64 (one_pass_lds(...) <= kMostLds)
+constexpr int kOnePassKeys = 256;
+constexpr size_t kMostLds = 156 * 1024;
+size_t one_pass_lds(const egeria_attention_desc *d, bool table_grad);
+hipError_t launch_attention_one_pass(const AttnArgs &a, egeria_dtype dt, bool vec, hipStream_t st);
 
 // a launcher's instance for the type, the head size and how the rows are read
 #define EG_PICK(go, a, dt, vec, st)                                                                              \
@@ -321,6 +327,54 @@ __device__ __forceinline__ void store4(T *row, int f, int dim, float x0, float x
     }
 }
 
+// The 32 rows of a wave, columns of a result across lanes (row i of the wave in lanes i and i + 32), times `by`, into rows t0 ... of a
+// tensor's head as far as `rows` goes.  VEC: through 32 rows of a tile in LDS that the wave has to itself (`lds`, its own after a
+// barrier), so that a request covers whole rows instead of 8 or 16 bytes of 32 of them: with those, the address unit worked a few
+// microseconds on a workgroup's results (forward of 64 x 256 x 12 x 64 STORE_US).
+template <typename T, int D, bool VEC>
+__device__ __forceinline__ void store_rows(const v16f (&x)[D / 32], float by, const View &v, int b, int h, int t0, int rows, int dim, uint32_t lds, int lane)
+{
+    typedef Tile<T, D> tile;
+    const int half = lane >> 5, mine = lane & 31;
+    T *base = (T *)v.p + ((int64_t)b * v.sb + (int64_t)h * v.sh);
+    if constexpr (!VEC) {
+        if (t0 + mine >= rows) return;
+#pragma unroll
+        for (int n = 0; n < D / 32; ++n)
+#pragma unroll
+            for (int r = 0; r < 16; r += 4)
+                store4<T, VEC>(base + (int64_t)(t0 + mine) * v.st, 32 * n + row_of(r, half), dim, x[n][r] * by, x[n][r + 1] * by, x[n][r + 2] * by, x[n][r + 3] * by);
+    } else {
+#pragma unroll
+        for (int n = 0; n < D / 32; ++n)
+#pragma unroll
+            for (int r = 0; r < 16; r += 4) {
+                const int f = 32 * n + row_of(r, half);
+                if constexpr (sizeof(T) == 2) {
+                    union { v2u w; __bf16 e[4]; } y;
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) y.e[e] = (__bf16)(x[n][r + e] * by);
+                    *(__attribute__((address_space(3))) v2u *)(uintptr_t)(lds + tile::at(mine, f >> 3) + 8 * half) = y.w;
+                } else {
+                    v4u y;
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) y[e] = __float_as_uint(x[n][r + e] * by);
+                    *(lds_v4u *)(uintptr_t)(lds + tile::at(mine, f >> 2)) = y;
+                }
+            }
+        wave_lds_turn();
+        constexpr int kPer = 64 / tile::kUnits;                             // rows of a request
+        const int u = lane % tile::kUnits;
+#pragma unroll
+        for (int n = 0; n < 32 / kPer; ++n) {
+            const int r = n * kPer + lane / tile::kUnits;
+            const v4u y = *(const lds_v4u *)(uintptr_t)(lds + tile::at(r, u));
+            if (t0 + r < rows && u * 16 < dim * (int)sizeof(T)) *(v4u *)((char *)(base + (int64_t)(t0 + r) * v.st) + u * 16) = y;
+        }
+        wave_lds_turn();
+    }
+}
+
 // The bias of one head by distance, in LDS: table entries in units of the scores' base-2 exponent (hidden ones minus infinity), from
 // distance -far - kPad to hi + kPad.  A block of at most 64 keys and 32 queries that reaches into [-far, hi] has no distance outside, so
 // its pairs are looked up without clamping, four neighbouring distances at a time; every other block has one bias for all of
@@ -331,28 +385,40 @@ __device__ __forceinline__ float table_value(const float *table, int row, int he
     const float t = table[row * heads + h];
     return t <= kHidden ? -INFINITY : t * kLog2e;
 }
-inline size_t bias_lut_floats(const AttnArgs &a) { return a.table ? align_up((size_t)distance_entries(a.b) + 2 * kPad, 4) : 0; }
+inline size_t bias_lut_floats(const Buckets &b) { return align_up((size_t)distance_entries(b) + 2 * kPad, 4) + 3 * kMaxBuckets; }
+inline size_t bias_lut_floats(const AttnArgs &a) { return a.table ? bias_lut_floats(a.b) : 0; }
 
 typedef float v4f_any __attribute__((ext_vector_type(4), aligned(4)));
 
 struct BiasLut {
     float *lut;
+    Span *spans;                            // entries of every bucket
+    float *value;
     int far, hi;                            // ends of the table: distances beyond them have the bias of the nearest end
     bool on;
 
+    __device__ __forceinline__ int count() const { return far + hi + 1 + 2 * kPad; }
+    __device__ __forceinline__ int room() const { return (count() + 3) & ~3; }
     __device__ __forceinline__ void open(const AttnArgs &a, float *memory)
     {
-        lut = memory;
         on = a.table != nullptr;
         far = a.b.far;
         hi = a.b.both ? a.b.far : 0;
+        lut = memory;
+        spans = (Span *)(lut + room());
+        value = (float *)(spans + kMaxBuckets);
+        if (on) find_spans(a.b, a.table_rows, kPad, spans);
     }
-    __device__ __forceinline__ int count() const { return far + hi + 1 + 2 * kPad; }
-    // by all 256 threads; the caller synchronises
-    __device__ __forceinline__ void fill(const AttnArgs &a, int h, int tid) const
+    __device__ __forceinline__ float *end() const { return value + kMaxBuckets; }
+    // by all threads: read(), a barrier, fill(); the caller synchronises after it
+    __device__ __forceinline__ void read(const AttnArgs &a, int h) const
     {
-        if (!on) return;
-        for (int n = tid; n < count(); n += 256) lut[n] = table_value(a.table, bucket_of_entry(a.b, distance_index(a.b, n - kPad - far)), a.heads, h);
+        if (on && (int)threadIdx.x < a.table_rows) value[threadIdx.x] = table_value(a.table, threadIdx.x, a.heads, h);
+    }
+    template <int THREADS = 256>
+    __device__ __forceinline__ void fill(const AttnArgs &a) const
+    {
+        if (on) each_entry<THREADS>(spans, a.table_rows, [&](int n, int e) { lut[e] = value[n]; });
     }
     // a block of pairs with distances lo ... top: one bias for all of them, which is it
     __device__ __forceinline__ bool left(int top) const { return top <= -far; }
@@ -367,7 +433,7 @@ inline hipError_t allow_lds(K kernel, size_t bytes, bool (&done)[kMaxDevices])
     const int dev = current_device();
     if (dev < 0) return hipErrorInvalidDevice;
     if (done[dev] || bytes <= 65536) return hipSuccess;
-    const hipError_t e = hipFuncSetAttribute((const void *)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, 156 * 1024);
+    const hipError_t e = hipFuncSetAttribute((const void *)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, (int)kMostLds);
     if (e == hipSuccess) done[dev] = true;
     return e;
 }

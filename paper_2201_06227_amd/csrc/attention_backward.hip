@@ -7,6 +7,7 @@
 //   dkv: S = Q K^T and dP = dO V^T (keys across), dV^T += dO^T P, dK^T += Q^T dS
 // In both, P and dS go from result to operand in registers (pack).
 #include "attention.hpp"
+#include "attention_diagonals.hpp"
 
 namespace egeria {
 
@@ -15,41 +16,6 @@ namespace {
 // Keys of a step of the dq kernel: half as many where a step would leave no LDS for the sums by distance.
 template <typename T, int D>
 constexpr int dq_keys() { return sizeof(T) * D == 512 ? kKeyTile / 2 : kKeyTile; }
-
-// Adds a block's dS^T (keys down, queries across) to sums by distance: into[d] for d = key - query of the block.
-// A value in lane l of a row of 16 lanes and register r has distance u - l, u being the register's key modulo 16, up to multiples of
-// 16 and of the half's 4 that all lanes of the row share.  Moved down by u lanes, values of one distance lie in one lane, those
-// that leave the row at the bottom come in at the top 16 distances further: two additions with a shift of lanes each, no LDS.  What
-// is left are the sums of 4 times 16 distances for each half of the wave, which has a table of its own: plain additions, in a
-// fixed order.  (As additions of all 1024 values in LDS, atomic ones that never collide, dq of 64 x 256 x 12 x 64 took 188 us, now
-// DQ_US.)
-template <int R>
-__device__ __forceinline__ void shift_add(const v16f &s, float (&a)[3])
-{
-    constexpr int key = 8 * (R >> 2) + (R & 3), u = key & 15, w = key >> 4;
-    const int x = __float_as_int(s[R]);
-    if constexpr (u == 0) a[w] += s[R];
-    else {
-        a[w] += __int_as_float(__builtin_amdgcn_update_dpp(0, x, 0x100 | u, 0xf, 0xf, true));                // lane i takes from i + u
-        a[w + 1] += __int_as_float(__builtin_amdgcn_update_dpp(0, x, 0x110 | (16 - u), 0xf, 0xf, true));     // from i - (16 - u)
-    }
-    if constexpr (R < 15) shift_add<R + 1>(s, a);
-}
-__device__ __forceinline__ void add_diagonals(const v16f &s, float *into, int lane)
-{
-    float a[3] = {0.0f, 0.0f, 0.0f};
-    shift_add<0>(s, a);
-    // a[v] of lane l: distance 16 v + 4 half - 16 (row of lanes in the half) - l % 16
-    const float up1 = lane_xor<16>(a[1]), up2 = lane_xor<16>(a[2]);
-    const bool low = !(lane & 16);
-    float *at = into + 4 * (lane >> 5) - (lane & 15);
-    const float x = low ? a[0] + up1 : a[0], y = a[1] + up2, z = a[2];
-    at[low ? 0 : -16] += x;
-    if (low) {
-        at[16] += y;
-        at[32] += z;
-    }
-}
 
 // ---- dq ---------------------------------------------------------------------------------------------------------
 
@@ -74,9 +40,9 @@ __global__ __launch_bounds__(256, sizeof(T) * D == 512 ? 1 : 2) void attention_d
     const uint32_t lds = (uint32_t)(uintptr_t)(lds_byte *)smem;
     BiasLut bias;
     bias.open(a, (float *)(smem + 4 * kTileBytes));
-    bias.fill(a, h, tid);
+    bias.read(a, h);
     const int entries = bias.count();
-    float *sums = bias.lut + ((entries + 3) & ~3);                          // [wave][half]: sums of ds by distance, laid out as the bias
+    float *sums = bias.end();                                               // [wave][half]: sums of ds by distance, laid out as the bias
     if (a.partials)
         for (int i = tid; i < 8 * entries; i += 256) sums[i] = 0.0f;
     float *mine = sums + (2 * wave + half) * entries;
@@ -111,6 +77,8 @@ __global__ __launch_bounds__(256, sizeof(T) * D == 512 ? 1 : 2) void attention_d
 #pragma unroll
     for (int n = 0; n < D / 32; ++n) dq[n] = v16f(0.0f);
     float left = 0.0f, right = 0.0f;                                        // sums of ds beyond the table by distance
+    if (bias.on) __syncthreads();
+    bias.fill(a);
 
     auto one_step = [&](auto buffer, int step) __attribute__((always_inline)) {
         constexpr uint32_t now = decltype(buffer)::value * 2 * kTileBytes, next = 2 * kTileBytes - now;
@@ -164,7 +132,7 @@ const int live = nk - jn - 4 * half, most = a.causal && -rel < live - 1 ? -rel +
                     for (int r = 0; r < 16; ++r) sum += s[r];
                     if (bias.left(hi)) left += sum;
                     else right += sum;
-                } else add_diagonals(s, mine + (jn - qw - shift + bias.far + kPad), lane);
+                } else add_diagonals<1>(s, mine + (jn - qw - shift + bias.far + kPad), lane);
             }
 #pragma unroll
             for (int k = 0; k < 2; ++k) {
@@ -179,20 +147,16 @@ const int live = nk - jn - 4 * half, most = a.causal && -rel < live - 1 ? -rel +
         if (step + 1 < steps) one_step(Const<1>(), step + 1);
     }
 
-    if (i < a.q_len) {
-        T *out = (T *)a.dq.p + ((int64_t)b * a.dq.sb + (int64_t)i * a.dq.st + (int64_t)h * a.dq.sh);
+    const float by = i < nq ? a.scale : 0.0f;
+    __syncthreads();                                                        // the tiles have been read
+    if (a.q_parts == 1) store_rows<T, D, VEC>(dq, by, a.dq, b, h, qw, a.q_len, a.dim, lds + 32 * wave * tile::kRowBytes, lane);
+    else if (i < a.q_len) {
         float *sum = a.part_q + (((int64_t)part * a.batch * a.heads + bh) * a.q_len + i) * D;
 #pragma unroll
         for (int n = 0; n < D / 32; ++n)
 #pragma unroll
-            for (int r = 0; r < 16; r += 4) {
-                const int f = 32 * n + row_of(r, half);
-                float x[4];
-#pragma unroll
-                for (int e = 0; e < 4; ++e) x[e] = i < nq ? dq[n][r + e] * a.scale : 0.0f;
-                if (a.q_parts > 1) *(float4 *)(sum + f) = make_float4(x[0], x[1], x[2], x[3]);
-                else store4<T, VEC>(out, f, a.dim, x[0], x[1], x[2], x[3]);
-            }
+            for (int r = 0; r < 16; r += 4)
+                *(float4 *)(sum + 32 * n + row_of(r, half)) = make_float4(dq[n][r] * by, dq[n][r + 1] * by, dq[n][r + 2] * by, dq[n][r + 3] * by);
     }
     if (a.partials) {
         left = wave_sum(left);
@@ -201,7 +165,7 @@ const int live = nk - jn - 4 * half, most = a.causal && -rel < live - 1 ? -rel +
             mine[0] += left;
             mine[entries - 1] += right;
         }
-        bucket_sums(a.b, sums, 8, entries, kPad, a.table_rows, a.partials + (((int64_t)h * a.batch + b) * a.q_parts * tiles + part * tiles + rt) * a.table_rows);
+        bucket_sums(bias.spans, sums, 8, entries, entries, a.table_rows, a.partials + (((int64_t)h * a.batch + b) * a.q_parts * tiles + part * tiles + rt) * a.table_rows);
     }
 }
 
@@ -225,8 +189,7 @@ __global__ __launch_bounds__(256, sizeof(T) * D == 512 ? 1 : 2) void attention_d
     // the table's gradient, whose partial sums the dq kernel has left: the first workgroups
     const uint32_t extra = a.dtable ? (uint32_t)a.heads : 0u;
     if (blockIdx.x < extra) {
-        const int64_t row_tiles = (a.q_len + kRowTile - 1) / kRowTile;
-        reduce_table<256>(a.partials, a.heads, (int64_t)a.batch * a.q_parts * row_tiles, a.table_rows, a.dtable, (int)blockIdx.x, (double *)smem);
+        reduce_table<256>(a.partials, a.heads, a.table_parts, a.table_rows, a.dtable, (int)blockIdx.x, (double *)smem);
         return;
     }
     const uint32_t tiles = (uint32_t)(a.k_len + kRowTile - 1) / kRowTile, piece = xcd_piece(blockIdx.x - extra, gridDim.x - extra);
@@ -303,7 +266,9 @@ __global__ __launch_bounds__(256, sizeof(T) * D == 512 ? 1 : 2) void attention_d
         asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
         __syncthreads();
         if (a.table && h != lut_head) {                                     // the next head of the group
-            bias.fill(a, h, tid);
+            bias.read(a, h);
+            __syncthreads();
+            bias.fill(a);
             lut_head = h;
             __syncthreads();
         }
@@ -364,29 +329,25 @@ __global__ __launch_bounds__(256, sizeof(T) * D == 512 ? 1 : 2) void attention_d
         if (step + 1 < steps) one_step(Const<1>(), step + 1);
     }
 
-    if (j < a.k_len) {
-        T *ok = (T *)a.dk.p + ((int64_t)b * a.dk.sb + (int64_t)j * a.dk.st + (int64_t)hk * a.dk.sh);
-        T *ov = (T *)a.dv.p + ((int64_t)b * a.dv.sb + (int64_t)j * a.dv.st + (int64_t)hk * a.dv.sh);
-        const bool live = j < nk;
+    __syncthreads();                                                        // the tiles have been read
+    if (!(j < nk)) {                                                        // (columns of their own, and anything may be in them)
+#pragma unroll
+        for (int n = 0; n < D / 32; ++n) dk[n] = dv[n] = v16f(0.0f);
+    }
+    if (a.kv_parts == 1) {
+        const uint32_t room = lds + 32 * wave * tile::kRowBytes;
+        store_rows<T, D, VEC>(dk, a.scale, a.dk, b, hk, jw, a.k_len, a.dim, room, lane);
+        store_rows<T, D, VEC>(dv, 1.0f, a.dv, b, hk, jw, a.k_len, a.dim, room, lane);
+    } else if (j < a.k_len) {
         float *sum = a.part_kv + (((int64_t)part * a.batch * a.kv_heads + bh) * a.k_len + j) * (2 * D);
+        const float by = a.scale;
 #pragma unroll
         for (int n = 0; n < D / 32; ++n)
 #pragma unroll
             for (int r = 0; r < 16; r += 4) {
                 const int f = 32 * n + row_of(r, half);
-                float x[4], y[4];
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    x[e] = live ? dk[n][r + e] * a.scale : 0.0f;
-                    y[e] = live ? dv[n][r + e] : 0.0f;
-                }
-                if (a.kv_parts > 1) {
-                    *(float4 *)(sum + f) = make_float4(x[0], x[1], x[2], x[3]);
-                    *(float4 *)(sum + D + f) = make_float4(y[0], y[1], y[2], y[3]);
-                } else {
-                    store4<T, VEC>(ok, f, a.dim, x[0], x[1], x[2], x[3]);
-                    store4<T, VEC>(ov, f, a.dim, y[0], y[1], y[2], y[3]);
-                }
+                *(float4 *)(sum + f) = make_float4(dk[n][r] * by, dk[n][r + 1] * by, dk[n][r + 2] * by, dk[n][r + 3] * by);
+                *(float4 *)(sum + D + f) = make_float4(dv[n][r], dv[n][r + 1], dv[n][r + 2], dv[n][r + 3]);
             }
     }
 }
@@ -427,7 +388,7 @@ hipError_t go_backward(const AttnArgs &a, hipStream_t st)
     const int64_t q_blocks = (int64_t)a.batch * a.heads * ((a.q_len + kRowTile - 1) / kRowTile) * a.q_parts;
     const int64_t k_blocks = (int64_t)a.batch * a.kv_heads * ((a.k_len + kRowTile - 1) / kRowTile) * a.kv_parts + (a.dtable ? a.heads : 0);
     if (q_blocks > 0) {
-        const size_t lds = 4 * dq_keys<T, D>() * row + 4 * lut * (a.partials ? 9 : 1);
+        const size_t lds = 4 * dq_keys<T, D>() * row + 4 * (lut + (a.partials ? 8 * ((size_t)distance_entries(a.b) + 2 * kPad) : 0));
         hipError_t e = allow_lds(attention_dq_kernel<T, D, VEC>, lds, done_q);
         if (e != hipSuccess) return e;
         e = launch_k(EGERIA_KERNEL_ATTENTION, attention_dq_kernel<T, D, VEC>, dim3((unsigned)q_blocks), dim3(256), lds, st, a);

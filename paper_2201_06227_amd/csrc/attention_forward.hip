@@ -101,7 +101,7 @@ __global__ __launch_bounds__(256, sizeof(T) * D == 512 ? 1 : 2) void attention_f
     const uint32_t lds = (uint32_t)(uintptr_t)(lds_byte *)smem;
     BiasLut bias;
     bias.open(a, (float *)(smem + 4 * kTileBytes));
-    bias.fill(a, h, tid);
+    bias.read(a, h);
 
     Rows<T, D, VEC> qr;
     qr.open(a.q, b, h, nq, a.dim);
@@ -119,6 +119,8 @@ __global__ __launch_bounds__(256, sizeof(T) * D == 512 ? 1 : 2) void attention_f
 #pragma unroll
     for (int kk = 0; kk < D / 16; ++kk) st.q[kk] = qr.frag(qw, kk, lane);
     const float c = a.scale * kLog2e;
+    if (bias.on) __syncthreads();
+    bias.fill(a);
 
     auto one_step = [&](auto buffer, int step) __attribute__((always_inline)) {
         constexpr uint32_t now = decltype(buffer)::value * 2 * kTileBytes, next = 2 * kTileBytes - now;
@@ -177,18 +179,11 @@ __global__ __launch_bounds__(256, sizeof(T) * D == 512 ? 1 : 2) void attention_f
         if (step + 1 < steps) one_step(Const<1>(), step + 1);
     }
 
-    const float total = st.l + lane_xor<32>(st.l);
-    if (i < a.q_len) {
-        const float l = i < nq ? total : 0.0f, inv = l > 0.0f ? 1.0f / l : 0.0f;
-        T *row = (T *)a.o.p + ((int64_t)b * a.o.sb + (int64_t)i * a.o.st + (int64_t)h * a.o.sh);
-#pragma unroll
-        for (int n = 0; n < D / 32; ++n)
-#pragma unroll
-            for (int r = 0; r < 16; r += 4)
-                store4<T, VEC>(row, 32 * n + row_of(r, half), a.dim, st.o[n][r] * inv, st.o[n][r + 1] * inv, st.o[n][r + 2] * inv, st.o[n][r + 3] * inv);
-        if (half == 0)
-            a.lse[((int64_t)b * a.heads + h) * a.q_len + i] = l > 0.0f ? (st.m + __builtin_amdgcn_logf(l)) * kLn2 : -INFINITY;
-    }
+    const float total = st.l + lane_xor<32>(st.l), l = i < nq ? total : 0.0f;
+    if (half == 0 && i < a.q_len)
+        a.lse[((int64_t)b * a.heads + h) * a.q_len + i] = l > 0.0f ? (st.m + __builtin_amdgcn_logf(l)) * kLn2 : -INFINITY;
+    __syncthreads();                                                        // the tiles have been read
+    store_rows<T, D, VEC>(st.o, l > 0.0f ? 1.0f / l : 0.0f, a.o, b, h, qw, a.q_len, a.dim, lds + 32 * wave * tile::kRowBytes, lane);
 }
 
 // ---- few rows ---------------------------------------------------------------------------------------------------
@@ -230,12 +225,15 @@ __global__ __launch_bounds__(256) void attention_few_kernel(AttnArgs a)
 
     const uint32_t lds = (uint32_t)(uintptr_t)(lds_byte *)smem + (uint32_t)wave * L::kWaveBytes;
     float *tab = (float *)(smem + L::kMain);                               // [heads of the tile][table rows]
-    uint8_t *lut = (uint8_t *)(tab + (h1 - h0 + 1) * a.table_rows);        // bucket of every distance
+    Span *spans = (Span *)(tab + (((h1 - h0 + 1) * a.table_rows + 1) & ~1));
+    uint8_t *lut = (uint8_t *)(spans + a.table_rows);                      // bucket of every distance
     const int lut_hi = a.b.both ? a.b.far : 0;
     if (a.table) {
         for (int n = tid; n < (h1 - h0 + 1) * a.table_rows; n += 256)
             tab[n] = table_value(a.table, n % a.table_rows, a.heads, g * a.group + h0 + n / a.table_rows);
-        for (int n = tid; n <= a.b.far + lut_hi; n += 256) lut[n] = (uint8_t)bucket_of_entry(a.b, n);
+        find_spans(a.b, a.table_rows, 0, spans);
+        __syncthreads();
+        each_entry(spans, a.table_rows, [&](int n, int e) { lut[e] = (uint8_t)n; });
     }
     const uint32_t r = r0 + (lane & 31), rr = r < rows ? r : rows - 1;
     const int hl = (int)(rr / (uint32_t)a.q_len), i = (int)(rr % (uint32_t)a.q_len), h = g * a.group + hl;
@@ -409,7 +407,7 @@ hipError_t go_few(const AttnArgs &a, hipStream_t st)
     static bool done[kMaxDevices] = {};
     const int64_t rows = (int64_t)a.group * a.q_len, tiles = (rows + kFewRows - 1) / kFewRows, all = (int64_t)a.batch * a.kv_heads * tiles;
     const int64_t heads = rows < kFewRows ? a.group : (kFewRows + a.q_len - 2) / a.q_len + 1;       // most heads of a tile
-    const size_t lds = FewLayout<T, D>::kMain + (a.table ? (size_t)heads * a.table_rows * 4 + align_up((size_t)distance_entries(a.b), 16) : 0);
+    const size_t lds = FewLayout<T, D>::kMain + (a.table ? (size_t)(heads * a.table_rows + 1) * 4 + a.table_rows * sizeof(Span) + align_up((size_t)distance_entries(a.b), 16) : 0);
     hipError_t e = allow_lds(attention_few_kernel<T, D, VEC>, lds, done);
     if (e != hipSuccess) return e;
     e = launch_k(EGERIA_KERNEL_ATTENTION, attention_few_kernel<T, D, VEC>, dim3((unsigned)(all * a.splits)), dim3(256), lds, st, a);

@@ -50,7 +50,13 @@ __global__ __launch_bounds__(256) void position_bias_kernel(Buckets b, const flo
     const uint32_t p = xcd_piece(blockIdx.x, gridDim.x);
     const uint32_t cb = p % deal.col_blocks, rb = p / deal.col_blocks % deal.row_blocks, h = p / deal.col_blocks / deal.row_blocks;
     const int entries = b.both ? 2 * b.far + 1 : b.far + 1;
-    for (int i = threadIdx.x; i < entries; i += 256) lut[spread(i)] = table[bucket_of_entry(b, i) * heads + h];
+    const int rows = b.both ? 2 * b.n : b.n;
+    Span *spans = (Span *)(lut + ((spread(entries) + 1) & ~1));
+    float *value = (float *)(spans + rows);
+    find_spans(b, rows, 0, spans);
+    if ((int)threadIdx.x < rows) value[threadIdx.x] = table[threadIdx.x * heads + h];
+    __syncthreads();
+    each_entry(spans, rows, [&](int n, int e) { lut[spread(e)] = value[n]; });
     __syncthreads();
     const int j0 = (int)((cb << deal.lg) + (threadIdx.x & ((1 << deal.lg) - 1))) * N;
     if (j0 >= k_len) return;
@@ -93,6 +99,8 @@ __global__ __launch_bounds__(256) void position_bias_backward_kernel(Buckets b, 
     const uint32_t cb = p % deal.col_blocks, rb = p / deal.col_blocks % deal.row_blocks, sh = p / deal.col_blocks / deal.row_blocks % deal.shares;
     const uint32_t h = p / deal.col_blocks / deal.row_blocks / deal.shares;
     const int entries = b.both ? 2 * b.far + 1 : b.far + 1;
+    Span *spans = (Span *)(sums + 8 * entries);
+    find_spans(b, rows_of_table, 0, spans);
     for (int i = threadIdx.x; i < 8 * entries; i += 256) sums[i] = 0.0f;
     __syncthreads();
     float *mine = sums + (threadIdx.x >> 5) * entries;
@@ -142,6 +150,7 @@ __global__ __launch_bounds__(256) void position_bias_backward_kernel(Buckets b, 
                 else if (rel >= hi) right += d[e];
                 else mine[rel + b.far] += d[e];
             }
+            wave_lds_turn();                                       // the next patch's lanes add where others of this one have
         }
     }
     left = wave_sum(left);
@@ -152,7 +161,7 @@ __global__ __launch_bounds__(256) void position_bias_backward_kernel(Buckets b, 
         mine[entries - 1] += right;
     }
     const int64_t part = ((int64_t)sh * deal.row_blocks + rb) * deal.col_blocks + cb, parts = (int64_t)deal.shares * deal.row_blocks * deal.col_blocks;
-    bucket_sums(b, sums, 8, entries, 0, rows_of_table, partials + ((int64_t)h * parts + part) * rows_of_table);
+    bucket_sums(spans, sums, 8, entries, entries, rows_of_table, partials + ((int64_t)h * parts + part) * rows_of_table);
 }
 
 constexpr int kReduceThreads = 1024;
@@ -195,12 +204,12 @@ bool valid_sizes(const egeria_position_table *t, int32_t heads, int32_t q_len, i
 
 int64_t parts_of(const Deal &p) { return (int64_t)p.shares * p.row_blocks * p.col_blocks; }
 
+}  // namespace
+
 hipError_t launch_table_reduce(const float *partials, int heads, int64_t parts, int buckets, float *dtable, hipStream_t st)
 {
     return launch_k(EGERIA_KERNEL_NONE, table_reduce_kernel, dim3((unsigned)heads), dim3(kReduceThreads), 0, st, partials, heads, parts, buckets, dtable);
 }
-
-}  // namespace
 
 }  // namespace egeria
 
@@ -219,7 +228,7 @@ egeria_status egeria_position_bias(const egeria_position_table *t, int32_t heads
     const int64_t blocks = parts_of(p) * heads;
     if (blocks > 0x7fffffffLL) return EGERIA_ERR_UNSUPPORTED;
     const int entries = distance_entries(b);
-    const size_t lds = 4 * (size_t)(entries + entries / 64 + 1);
+    const size_t lds = 4 * (size_t)(entries + entries / 64 + 2) + t->buckets * (sizeof(Span) + 4);
     auto go = [&](auto kernel, auto *out) {
         return launch_k(EGERIA_KERNEL_NONE, kernel, dim3((unsigned)blocks), dim3(256), lds, (hipStream_t)stream, b, t->table, (int)heads,
                         (int)q_len, (int)k_len, (int)offset, p, out);
@@ -252,7 +261,7 @@ egeria_status egeria_position_bias_backward(const egeria_position_table *t, cons
     const Deal p = make_deal(batch, heads, q_len, k_len, dt == EGERIA_F32 ? 4 : 8, true);
     const int64_t blocks = parts_of(p) * heads;
     if (blocks > 0x7fffffffLL) return EGERIA_ERR_UNSUPPORTED;
-    const size_t lds = 32 * (size_t)distance_entries(b);
+    const size_t lds = 32 * (size_t)distance_entries(b) + t->buckets * sizeof(Span);
     auto go = [&](auto kernel, auto *src) {
         return launch_k(EGERIA_KERNEL_NONE, kernel, dim3((unsigned)blocks), dim3(256), lds, st, b, src, (int64_t)batch, (int)heads, (int)q_len,
                         (int)k_len, (int)offset, p, (int)t->buckets, partials);

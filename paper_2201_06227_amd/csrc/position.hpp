@@ -58,17 +58,6 @@ __device__ __forceinline__ int distance_index(const Buckets &b, int rel)
     const int hi = b.both ? b.far : 0;
     return (rel < -b.far ? -b.far : (rel > hi ? hi : rel)) + b.far;
 }
-// bucket of entry `at` of the table by distance
-__device__ __forceinline__ int bucket_of_entry(const Buckets &b, int at)
-{
-    const int rel = at - b.far, dist = rel < 0 ? -rel : rel;
-    int k = dist;
-    if (dist >= b.e) {
-        k = b.e;
-        for (int i = 1; i < b.n - b.e; ++i) k += dist >= b.border[i] ? 1 : 0;
-    }
-    return rel > 0 ? b.n + k : k;           // (one-sided tables have no entry beyond 0)
-}
 // First entry of the table by distance that bucket `row` holds, and how many (0: none)
 __device__ __forceinline__ int entries_of_bucket(const Buckets &b, int row, int *count)
 {
@@ -82,27 +71,50 @@ __device__ __forceinline__ int entries_of_bucket(const Buckets &b, int row, int 
     return right ? b.far + lo : b.far - hi + 1;
 }
 
-// What a workgroup of 256 threads makes of sums by distance: copies [copies][stride] in LDS, of entries -far - pad ... hi + pad each, to
-// the sums by bucket out[0 .. rows).  Distances beyond the table's ends belong to the ends' buckets.
-__device__ __forceinline__ void bucket_sums(const Buckets &b, float *sums, int copies, int stride, int pad, int rows, float *out)
+// The entries of every bucket in a table by distance with `pad` more entries on each side, which belong to the ends' buckets, into LDS:
+// by the first `rows` of the workgroup's threads, all borders in one round trip.  (Looked up where they were needed, one bucket
+// after the other, they took most of a short call's time: dq of 64 x 256 x 12 x 64 57 us, now DQ_SPANS.)
+struct Span {
+    int at, count;
+};
+__device__ __forceinline__ void find_spans(const Buckets &b, int rows, int pad, Span *spans)
 {
-    const int entries = b.far + (b.both ? b.far : 0) + 1, tid = threadIdx.x, lane = tid & 63;
+    if ((int)threadIdx.x >= rows) return;
+    const int entries = b.far + (b.both ? b.far : 0) + 1;
+    int count, at = entries_of_bucket(b, threadIdx.x, &count);
+    if (count > 0) {
+        if (at + count == entries) count += pad;
+        if (at == 0) count += pad;
+        else at += pad;
+    }
+    spans[threadIdx.x] = {at, count};
+}
+// For every bucket f(bucket, entry) of each of its entries: a wave for each bucket in turn
+template <int THREADS = 256, typename F>
+__device__ __forceinline__ void each_entry(const Span *spans, int rows, F f)
+{
+    for (int n = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6); n < rows; n += THREADS / 64) {
+        const Span s = spans[n];
+        for (int e = threadIdx.x & 63; e < s.count; e += 64) f(n, s.at + e);
+    }
+}
+
+// What a workgroup makes of sums by distance, copies [copies][stride] in LDS of `entries` each, to the sums by bucket out[0 .. rows).
+template <int THREADS = 256>
+__device__ __forceinline__ void bucket_sums(const Span *spans, float *sums, int copies, int stride, int entries, int rows, float *out)
+{
+    const int tid = threadIdx.x, lane = tid & 63;
     __syncthreads();
-    for (int e = tid; e < entries + 2 * pad; e += 256) {
+    for (int e = tid; e < entries; e += THREADS) {
         float s = sums[e];
         for (int w = 1; w < copies; ++w) s += sums[w * stride + e];
         sums[e] = s;
     }
     __syncthreads();
-    for (int n = tid >> 6; n < rows; n += 4) {
-        int count, at = entries_of_bucket(b, n, &count);
-        if (count > 0) {
-            if (at + count == entries) count += pad;
-            if (at == 0) count += pad;
-            else at += pad;
-        }
+    for (int n = tid >> 6; n < rows; n += THREADS / 64) {
+        const Span r = spans[n];
         float s = 0.0f;
-        for (int e = lane; e < count; e += 64) s += sums[at + e];
+        for (int e = lane; e < r.count; e += 64) s += sums[r.at + e];
         s = wave_sum(s);
         if (lane == 0) out[n] = s;
     }
@@ -137,5 +149,8 @@ __device__ __forceinline__ void reduce_table(const float *__restrict__ partials,
     }
 }
 #endif
+
+// dtable of partial sums [heads][parts][buckets] (reduce_table)
+hipError_t launch_table_reduce(const float *partials, int heads, int64_t parts, int buckets, float *dtable, hipStream_t st);
 
 }  // namespace egeria

@@ -269,6 +269,24 @@ def test_attention_lengths(eg, dtype, causal, with_bias):
 
 @pytest.mark.gpu
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("shape,causal,bias,lens", [
+    ((64, 40, 33, 2, 2, 64), False, None, False), ((32, 70, 130, 8, 4, 40), True, None, True), ((43, 130, 200, 3, 3, 64), False, (32, 128, True), True),
+    ((130, 5, 256, 1, 1, 33), False, (16, 40, True), False), ((16, 100, 128, 16, 8, 64), True, (32, 128, False), True), ((128, 1, 1, 1, 1, 1), False, None, False),
+    ((64, 64, 255, 2, 2, 16), True, (8, 20, True), True), ((32, 300, 64, 4, 4, 48), True, (32, 100, False), True), ((26, 200, 256, 10, 5, 64), False, (20, 50, True), True),
+    ((64, 33, 100, 2, 2, 64), False, (4, 1024, True), False)], ids=str)
+def test_attention_many_short_sequences(eg, dtype, shape, causal, bias, lens):
+    """Batches with a workgroup for each key head: few keys, queries of every number, shared key heads, empty sequences."""
+    b, nq, nk, h = shape[:4]
+    rng = np.random.default_rng(b + nk)
+    ql, kl = (rng.integers(0, nq + 1, b), rng.integers(0, nk + 1, b)) if lens else (None, None)
+    if lens:
+        ql[:4], kl[:4] = [nq, 0, nq, nq], [nk, nk, 0, 1]
+    tab = None if bias is None else (table(bias[0], h), bias[1], bias[2])
+    run_and_check(eg, dtype, *make(dtype, *shape, seed=b), causal=causal, bias=tab, q_lens=None if ql is None else ql.tolist(), k_lens=None if kl is None else kl.tolist())
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
 def test_attention_does_not_read_padding(eg, dtype):
     """What lies behind a sequence's length may hold anything."""
     q, k, v, dout = make(dtype, 3, 40, 90, 2, 2, 64, seed=11)
