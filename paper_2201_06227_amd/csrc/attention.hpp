@@ -63,6 +63,25 @@ typedef __attribute__((address_space(3))) v4s lds_v4s;
 typedef __attribute__((address_space(3))) v4u lds_v4u;
 typedef __attribute__((address_space(3))) float lds_f32;
 
+// Which piece of the launch a workgroup takes.  Its `units` (sequences, or shares of their keys) have `per` pieces each: a unit's pieces
+// go to one XCD, where the rows of keys that several of them read are in its L2 and heads that lie side by side in memory are read at
+// the same time; neighbouring units, which are as long as each other where the batch is sorted by length, go to different XCDs
+// (workgroup ids go round the 8 XCDs).  The units left over when eight at a time have been dealt are spread over all XCDs.
+// DEAL_MEASURE
+struct Piece {
+    uint32_t unit, rest;
+};
+__device__ __forceinline__ Piece deal_units(uint32_t blk, uint32_t units, uint32_t per)
+{
+    const uint32_t even = units & ~7u;
+    if (blk < even * per) {
+        const uint32_t n = blk >> 3, u = n / per;
+        return {u * 8 + (blk & 7u), n - u * per};
+    }
+    const uint32_t n = xcd_piece(blk - even * per, (units - even) * per), u = n / per;
+    return {even + u, n - u * per};
+}
+
 struct v8f {
     float v[8];
 };

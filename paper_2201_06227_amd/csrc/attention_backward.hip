@@ -26,10 +26,11 @@ __global__ __launch_bounds__(256, sizeof(T) * D == 512 ? 1 : 2) void attention_d
     typedef Tile<T, D> tile;
     constexpr int kKeys = dq_keys<T, D>(), kTileBytes = kKeys * tile::kRowBytes;
     const int tid = threadIdx.x, lane = tid & 63, half = lane >> 5, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const uint32_t tiles = (uint32_t)(a.q_len + kRowTile - 1) / kRowTile, piece = xcd_piece(blockIdx.x, gridDim.x);
-    const uint32_t rt = tiles - 1 - piece % tiles;                          // the longest rows of a causal head first
-    const int part = (int)(piece / tiles % (uint32_t)a.q_parts), bh = (int)(piece / tiles / (uint32_t)a.q_parts);
-    const int q0 = (int)rt * kRowTile, h = bh % a.heads, b = bh / a.heads;
+    const uint32_t tiles = (uint32_t)(a.q_len + kRowTile - 1) / kRowTile;
+    const Piece piece = deal_units(blockIdx.x, (uint32_t)a.batch, (uint32_t)(a.heads * a.q_parts) * tiles);
+    const uint32_t rt = tiles - 1 - piece.rest % tiles;                     // the longest rows of a causal head first
+    const int part = (int)(piece.rest / tiles % (uint32_t)a.q_parts), b = (int)piece.unit, h = (int)(piece.rest / tiles / (uint32_t)a.q_parts);
+    const int q0 = (int)rt * kRowTile, bh = b * a.heads + h;
     const int nq = clamped(a.q_lens, b, a.q_len), nk = clamped(a.k_lens, b, a.k_len), shift = a.causal ? nk - nq : 0;
     const int rows = nq - q0 < kRowTile ? nq - q0 : kRowTile;
     int keys = rows > 0 ? nk : 0;
@@ -192,9 +193,10 @@ __global__ __launch_bounds__(256, sizeof(T) * D == 512 ? 1 : 2) void attention_d
         reduce_table<256>(a.partials, a.heads, a.table_parts, a.table_rows, a.dtable, (int)blockIdx.x, (double *)smem);
         return;
     }
-    const uint32_t tiles = (uint32_t)(a.k_len + kRowTile - 1) / kRowTile, piece = xcd_piece(blockIdx.x - extra, gridDim.x - extra);
-    const int part = (int)(piece / tiles % (uint32_t)a.kv_parts), bh = (int)(piece / tiles / (uint32_t)a.kv_parts);
-    const int k0 = (int)(piece % tiles) * kRowTile, hk = bh % a.kv_heads, b = bh / a.kv_heads;
+    const uint32_t tiles = (uint32_t)(a.k_len + kRowTile - 1) / kRowTile;
+    const Piece piece = deal_units(blockIdx.x - extra, (uint32_t)a.batch, (uint32_t)(a.kv_heads * a.kv_parts) * tiles);
+    const int part = (int)(piece.rest / tiles % (uint32_t)a.kv_parts), b = (int)piece.unit, hk = (int)(piece.rest / tiles / (uint32_t)a.kv_parts);
+    const int k0 = (int)(piece.rest % tiles) * kRowTile, bh = b * a.kv_heads + hk;
     const int nq = clamped(a.q_lens, b, a.q_len), nk = clamped(a.k_lens, b, a.k_len), shift = a.causal ? nk - nq : 0;
     // queries that see a key of the tile: from `first` on; the same for every head of the group
     int first = a.causal && k0 > shift ? (k0 - shift) / kQueries * kQueries : 0;

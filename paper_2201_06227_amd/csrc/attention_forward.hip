@@ -89,9 +89,10 @@ __global__ __launch_bounds__(256, sizeof(T) * D == 512 ? 1 : 2) void attention_f
     typedef Tile<T, D> tile;
     constexpr int kTileBytes = kKeyTile * tile::kRowBytes;
     const int tid = threadIdx.x, lane = tid & 63, half = lane >> 5, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const uint32_t tiles = (uint32_t)(a.q_len + kRowTile - 1) / kRowTile, piece = xcd_piece(blockIdx.x, gridDim.x);
+    const uint32_t tiles = (uint32_t)(a.q_len + kRowTile - 1) / kRowTile;
+    const Piece piece = deal_units(blockIdx.x, (uint32_t)a.batch, (uint32_t)a.heads * tiles);
     // the longest rows of a causal head first
-    const int q0 = (int)(tiles - 1 - piece % tiles) * kRowTile, h = (int)(piece / tiles % (uint32_t)a.heads), b = (int)(piece / tiles / (uint32_t)a.heads);
+    const int q0 = (int)(tiles - 1 - piece.rest % tiles) * kRowTile, h = (int)(piece.rest / tiles), b = (int)piece.unit;
     const int nq = clamped(a.q_lens, b, a.q_len), nk = clamped(a.k_lens, b, a.k_len), shift = a.causal ? nk - nq : 0;
     const int rows = nq - q0 < kRowTile ? nq - q0 : kRowTile;               // live rows of the tile (may be negative)
     int keys = rows > 0 ? nk : 0;
@@ -209,8 +210,9 @@ __global__ __launch_bounds__(256) void attention_few_kernel(AttnArgs a)
     __shared__ float stat[2][4][kFewRows];
     const int tid = threadIdx.x, lane = tid & 63, half = lane >> 5, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const uint32_t rows = (uint32_t)a.group * (uint32_t)a.q_len, tiles = (rows + kFewRows - 1) / kFewRows;
-    const uint32_t piece = xcd_piece(blockIdx.x, gridDim.x), split = piece % (uint32_t)a.splits, rt = piece / (uint32_t)a.splits % tiles;
-    const int g = (int)(piece / (uint32_t)a.splits / tiles % (uint32_t)a.kv_heads), b = (int)(piece / (uint32_t)a.splits / tiles / (uint32_t)a.kv_heads);
+    const Piece piece = deal_units(blockIdx.x, (uint32_t)(a.batch * a.splits), tiles * (uint32_t)a.kv_heads);
+    const uint32_t split = piece.unit % (uint32_t)a.splits, rt = piece.rest / (uint32_t)a.kv_heads;
+    const int g = (int)(piece.rest % (uint32_t)a.kv_heads), b = (int)(piece.unit / (uint32_t)a.splits);
     const int nq = clamped(a.q_lens, b, a.q_len), nk = clamped(a.k_lens, b, a.k_len), shift = a.causal ? nk - nq : 0;
     const uint32_t r0 = rt * kFewRows, r1 = r0 + kFewRows < rows ? r0 + kFewRows : rows;
     const int h0 = (int)(r0 / (uint32_t)a.q_len), h1 = (int)((r1 - 1) / (uint32_t)a.q_len);        // heads of the group in this tile
@@ -346,7 +348,7 @@ __global__ __launch_bounds__(256) void attention_few_kernel(AttnArgs a)
             store4<T, VEC>(out, f, a.dim, o[0] * inv, o[1] * inv, o[2] * inv, o[3] * inv);
             if (f == 0) a.lse[((int64_t)b * a.heads + head) * a.q_len + qi] = l > 0.0f ? (top + __builtin_amdgcn_logf(l)) * kLn2 : -INFINITY;
         } else {
-            const int64_t at = (int64_t)piece * kFewRows + row;
+            const int64_t at = ((((int64_t)b * a.kv_heads + g) * tiles + rt) * a.splits + split) * kFewRows + row;
             *(float4 *)(a.split_o + at * D + f) = make_float4(o[0], o[1], o[2], o[3]);
             if (f == 0) {
                 a.split_ml[2 * at] = top;
@@ -370,18 +372,36 @@ __global__ __launch_bounds__(256) void attention_join_kernel(AttnArgs a, uint32_
     const int b = (int)(bg / a.kv_heads), g = (int)(bg % a.kv_heads);
     const int head = g * a.group + (int)(row / (uint32_t)a.q_len), qi = (int)(row % (uint32_t)a.q_len);
     const int64_t at = tile * a.splits * kFewRows + n % kFewRows;
-    float top = -INFINITY;
-    for (int s = 0; s < a.splits; ++s) top = fmaxf(top, a.split_ml[2 * (at + (int64_t)s * kFewRows)]);
-    float l = 0.0f, o[4] = {0.0f, 0.0f, 0.0f, 0.0f};
-    for (int s = 0; s < a.splits; ++s) {
-        const int64_t p = at + (int64_t)s * kFewRows;
-        const float k = top == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(a.split_ml[2 * p] - top);
-        const float4 x = *(const float4 *)(a.split_o + p * D + f);
-        l = fmaf(a.split_ml[2 * p + 1], k, l);
-        o[0] = fmaf(x.x, k, o[0]);
-        o[1] = fmaf(x.y, k, o[1]);
-        o[2] = fmaf(x.z, k, o[2]);
-        o[3] = fmaf(x.w, k, o[3]);
+    // eight splits at a time, their statistics and values asked for together
+    float top = -INFINITY, l = 0.0f, o[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+    for (int s0 = 0; s0 < a.splits; s0 += 8) {
+        float2 ml[8];
+        float4 x[8];
+#pragma unroll
+        for (int s = 0; s < 8; ++s) {
+            const int64_t p = at + (int64_t)(s0 + s < a.splits ? s0 + s : s0) * kFewRows;
+            ml[s] = *(const float2 *)(a.split_ml + 2 * p);
+            x[s] = *(const float4 *)(a.split_o + p * D + f);
+            if (s0 + s >= a.splits) ml[s] = make_float2(-INFINITY, 0.0f);
+        }
+        float to = top;
+#pragma unroll
+        for (int s = 0; s < 8; ++s) to = fmaxf(to, ml[s].x);
+        if (to == -INFINITY) continue;
+        const float keep = __builtin_amdgcn_exp2f(top - to);
+        l *= keep;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) o[e] *= keep;
+        top = to;
+#pragma unroll
+        for (int s = 0; s < 8; ++s) {
+            const float k = __builtin_amdgcn_exp2f(ml[s].x - top);
+            l = fmaf(ml[s].y, k, l);
+            o[0] = fmaf(x[s].x, k, o[0]);
+            o[1] = fmaf(x[s].y, k, o[1]);
+            o[2] = fmaf(x[s].z, k, o[2]);
+            o[3] = fmaf(x[s].w, k, o[3]);
+        }
     }
     if (qi >= clamped(a.q_lens, b, a.q_len)) l = 0.0f;
     const float inv = l > 0.0f ? 1.0f / l : 0.0f;
