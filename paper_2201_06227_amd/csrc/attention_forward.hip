@@ -32,10 +32,21 @@ struct RowState {
     {
 #pragma unroll
         for (int n = 0; n < N; ++n) s[n] = v16f(0.0f);
+        if constexpr (N == 1) {
+            // a chain of its own for every other product: with one, a wave alone on its SIMD waits for each to end
+            v16f odd = v16f(0.0f);
 #pragma unroll
-        for (int kk = 0; kk < kDepth; ++kk)
+            for (int kk = 0; kk < kDepth; kk += 2) {
+                s[0] = mma(tile::row_frag(at, k_off, 0, kk), q[kk], s[0]);
+                odd = mma(tile::row_frag(at, k_off, 0, kk + 1), q[kk + 1], odd);
+            }
+            s[0] += odd;
+        } else {
 #pragma unroll
-            for (int n = 0; n < N; ++n) s[n] = mma(tile::row_frag(at, k_off, 32 * n, kk), q[kk], s[n]);
+            for (int kk = 0; kk < kDepth; ++kk)
+#pragma unroll
+                for (int n = 0; n < N; ++n) s[n] = mma(tile::row_frag(at, k_off, 32 * n, kk), q[kk], s[n]);
+        }
     }
     // The reference that exponents are taken against after a step with maximum `top` (both lanes of a query agree on it).  It follows
     // the maximum only when that has grown by more than kSlack: until then p <= 2^kSlack, which costs neither fp32 sums nor bf16
@@ -255,6 +266,7 @@ __global__ __launch_bounds__(256) void attention_few_kernel(AttnArgs a)
     vr.open(a.v, b, g, nk, a.dim, lane);
     const typename Tile<T, D>::Lane at_lane = Tile<T, D>::lane_at(lds, lane);
     if (a.table) __syncthreads();
+    const float beta_left = a.table ? my_tab[lut[0]] : 0.0f, beta_right = a.table ? my_tab[lut[a.b.far + lut_hi]] : 0.0f;
     constexpr int kLoads = 2 * kFewKeys * Tile<T, D>::kUnits / 64;         // requests of one step
     int j0 = k0 + kFewKeys * wave;
     auto stage = [&](uint32_t to, int j) {
@@ -278,12 +290,12 @@ __global__ __launch_bounds__(256) void attention_few_kernel(AttnArgs a)
         st.scores(s, at_lane, now);
         const int rel = j0 - i - shift;                                     // distances rel ... rel + 31
         const bool edge = j0 + kFewKeys > nk || (a.causal && __any(rel + kFewKeys - 1 > 0));
-        float beta = 0.0f;
+        float beta = beta_right;
         bool far = true;
         if (a.table) {
             const bool left = rel + kFewKeys - 1 <= -a.b.far, right = rel >= lut_hi;
             far = __all(left || right);
-            beta = my_tab[lut[left ? 0 : a.b.far + lut_hi]];
+            if (left) beta = beta_left;
         }
 #pragma unroll
         for (int e = 0; e < 16; ++e) {

@@ -34,9 +34,11 @@ template <> __device__ __forceinline__ uint16_t narrow<uint16_t>(float v)
 }
 
 // Where a thread's patches lie: 2^lg units of 16 bytes side by side (32 to 256 of them, so that half a wave has one row of patches),
-// 256 / 2^lg patches below each other, `rows` rows to a workgroup.
+// 256 / 2^lg patches below each other: `rows` rows to a workgroup, and `cols` times these columns one after the other, so that what
+// a workgroup writes or reads lies close together (long rows in pieces of 4 KiB, 64 of them below each other, were written at
+// 4.9 TB/s; 8 whole rows of 8 KiB at WRITE_RATE).
 struct Deal {
-    int lg, rows;
+    int lg, rows, cols;
     uint32_t row_blocks, col_blocks, shares;
 };
 
@@ -58,10 +60,11 @@ __global__ __launch_bounds__(256) void position_bias_kernel(Buckets b, const flo
     __syncthreads();
     each_entry(spans, rows, [&](int n, int e) { lut[spread(e)] = value[n]; });
     __syncthreads();
-    const int j0 = (int)((cb << deal.lg) + (threadIdx.x & ((1 << deal.lg) - 1))) * N;
-    if (j0 >= k_len) return;
+    const int i0 = (int)rb * deal.rows + (int)(threadIdx.x >> deal.lg) * kRows;
     const int last = (int)rb * deal.rows + deal.rows < q_len ? (int)rb * deal.rows + deal.rows : q_len;
-    for (int i0 = (int)rb * deal.rows + (int)(threadIdx.x >> deal.lg) * kRows; i0 < last; i0 += kRows << (8 - deal.lg)) {
+    for (int c = 0; c < deal.cols; ++c) {
+        const int j0 = (int)(((cb * deal.cols + c) << deal.lg) + (threadIdx.x & ((1 << deal.lg) - 1))) * N;
+        if (j0 >= k_len) return;
         T v[kRows + N - 1];                                        // distances first, first + 1, ...
         const int first = j0 - (i0 + kRows - 1) - offset;
 #pragma unroll
@@ -105,15 +108,16 @@ __global__ __launch_bounds__(256) void position_bias_backward_kernel(Buckets b, 
     __syncthreads();
     float *mine = sums + (threadIdx.x >> 5) * entries;
     const int64_t b0 = batch * sh / deal.shares, b1 = batch * (sh + 1) / deal.shares;
-    const int j0 = (int)((cb << deal.lg) + (threadIdx.x & ((1 << deal.lg) - 1))) * N;
+    const int i0 = (int)rb * deal.rows + (int)(threadIdx.x >> deal.lg) * kRows;
     const int last = (int)rb * deal.rows + deal.rows < q_len ? (int)rb * deal.rows + deal.rows : q_len;
     float left = 0.0f, right = 0.0f;                               // patches whose distances all lie beyond the table
     const int hi = b.both ? b.far : 0;
-    for (int i0 = (int)rb * deal.rows + (int)(threadIdx.x >> deal.lg) * kRows; i0 < last; i0 += kRows << (8 - deal.lg)) {
+    for (int c = 0; c < deal.cols; ++c) {
+        const int j0 = (int)(((cb * deal.cols + c) << deal.lg) + (threadIdx.x & ((1 << deal.lg) - 1))) * N;
         float d[kRows + N - 1];
 #pragma unroll
         for (int e = 0; e < kRows + N - 1; ++e) d[e] = 0.0f;
-        if (j0 < k_len)
+        if (j0 < k_len && i0 < last)
             for (int64_t n = b0; n < b1; ++n) {
                 const T *src = dbias + ((n * heads + h) * q_len + i0) * k_len + j0;
                 vec w[kRows];
@@ -172,26 +176,24 @@ __global__ __launch_bounds__(kReduceThreads) void table_reduce_kernel(const floa
     reduce_table<kReduceThreads>(partials, heads, parts, buckets, dtable, blockIdx.x, memory);
 }
 
-// How rows, columns and, for the gradient, the batch are dealt to workgroups: one patch for each thread, more rows where that still
-// leaves 2048 workgroups, and the batch in shares where rows and columns alone do not give 1024.
-Deal make_deal(int64_t batch, int heads, int q_len, int k_len, int per_unit, bool split_batch)
+// How rows, columns and, for the gradient, the batch are dealt to workgroups: one row of patches for each thread, up to four pieces of
+// the columns where that leaves 2048 workgroups, and the batch in shares where rows and columns alone do not give 1024.
+Deal make_deal(int64_t batch, int heads, int q_len, int k_len, int per_unit)
 {
     Deal p;
     const int64_t units = ((int64_t)k_len + per_unit - 1) / per_unit;
     p.lg = 5;
     while (p.lg < 8 && (1 << p.lg) < units) ++p.lg;
-    p.col_blocks = (uint32_t)((units + (1 << p.lg) - 1) >> p.lg);
     p.rows = kRows << (8 - p.lg);
-    auto blocks = [&](int rows) { return ((int64_t)q_len + rows - 1) / rows * p.col_blocks * heads; };
-    for (int n = 0; n < 3 && blocks(2 * p.rows) >= 2048; ++n) p.rows *= 2;
     p.row_blocks = (uint32_t)(((int64_t)q_len + p.rows - 1) / p.rows);
-    int64_t shares = 1;
-    if (split_batch) {
-        shares = blocks(p.rows) > 0 ? (1024 + blocks(p.rows) - 1) / blocks(p.rows) : 1;
-        shares = shares > batch ? batch : shares;
-        shares = shares < 1 ? 1 : shares;
-    }
-    p.shares = (uint32_t)shares;
+    const int64_t pieces = (units + (1 << p.lg) - 1) >> p.lg, rows = (int64_t)p.row_blocks * heads;
+    p.cols = 1;
+    while (p.cols < 4 && p.cols < pieces && (pieces + p.cols) / (p.cols + 1) * rows >= 2048) ++p.cols;
+    p.col_blocks = (uint32_t)((pieces + p.cols - 1) / p.cols);
+    const int64_t blocks = p.col_blocks * rows;
+    int64_t shares = blocks > 0 ? (1024 + blocks - 1) / blocks : 1;
+    shares = shares > batch ? batch : shares;
+    p.shares = (uint32_t)(shares < 1 ? 1 : shares);
     return p;
 }
 
@@ -224,8 +226,8 @@ egeria_status egeria_position_bias(const egeria_position_table *t, int32_t heads
     if (q_len == 0 || k_len == 0) return EGERIA_OK;
     if (!bias || ((uintptr_t)bias & 15u)) return EGERIA_ERR_INVALID_ARG;
     const Buckets b = make_buckets(t);
-    const Deal p = make_deal(1, heads, q_len, k_len, dt == EGERIA_F32 ? 4 : 8, false);
-    const int64_t blocks = parts_of(p) * heads;
+    const Deal p = make_deal(1, heads, q_len, k_len, dt == EGERIA_F32 ? 4 : 8);
+    const int64_t blocks = (int64_t)p.row_blocks * p.col_blocks * heads;
     if (blocks > 0x7fffffffLL) return EGERIA_ERR_UNSUPPORTED;
     const int entries = distance_entries(b);
     const size_t lds = 4 * (size_t)(entries + entries / 64 + 2) + t->buckets * (sizeof(Span) + 4);
@@ -241,7 +243,7 @@ size_t egeria_position_bias_workspace_bytes(const egeria_position_table *t, int3
                                             egeria_dtype dt)
 {
     if (!valid_sizes(t, heads, q_len, k_len, 0, dt) || batch < 0) return 0;
-    const Deal p = make_deal(batch, heads, q_len, k_len, dt == EGERIA_F32 ? 4 : 8, true);
+    const Deal p = make_deal(batch, heads, q_len, k_len, dt == EGERIA_F32 ? 4 : 8);
     return align_up((size_t)parts_of(p) * heads * t->buckets * 4, 256) + 256;
 }
 
@@ -258,7 +260,7 @@ egeria_status egeria_position_bias_backward(const egeria_position_table *t, cons
     float *partials = (float *)ws;
     if (none) return launch_table_reduce(partials, heads, 0, t->buckets, dtable, st) == hipSuccess ? EGERIA_OK : EGERIA_ERR_HIP;
     const Buckets b = make_buckets(t);
-    const Deal p = make_deal(batch, heads, q_len, k_len, dt == EGERIA_F32 ? 4 : 8, true);
+    const Deal p = make_deal(batch, heads, q_len, k_len, dt == EGERIA_F32 ? 4 : 8);
     const int64_t blocks = parts_of(p) * heads;
     if (blocks > 0x7fffffffLL) return EGERIA_ERR_UNSUPPORTED;
     const size_t lds = 32 * (size_t)distance_entries(b) + t->buckets * sizeof(Span);

@@ -19,7 +19,7 @@ struct Buckets {
     int32_t e;                              // distances below e have buckets of their own
     int32_t both;                           // the two sides have buckets of their own
     int32_t far;                            // first distance of the last bucket
-    int32_t border[kMaxBuckets];            // first distance of bucket e + k
+    int16_t border[kMaxBuckets];            // first distance of bucket e + k (launch arguments are copied: as short as they can be)
 };
 
 inline int position_rows(const egeria_position_table *t) { return t ? t->buckets : 0; }
@@ -40,10 +40,10 @@ inline Buckets make_buckets(const egeria_position_table *t)
     b.n = b.both ? t->buckets / 2 : t->buckets;
     b.e = b.n / 2;
     const int m = b.n - b.e;
-    for (int k = 0; k < kMaxBuckets; ++k) b.border[k] = 0x7fffffff;
+    for (int k = 0; k < kMaxBuckets; ++k) b.border[k] = 0x7fff;
     for (int k = 0; k < m; ++k) {
         const double x = (double)b.e * pow((double)t->max_distance / b.e, (double)k / m), near = rint(x);
-        b.border[k] = (int32_t)(fabs(x - near) <= 1e-12 * x ? near : ceil(x));
+        b.border[k] = (int16_t)(fabs(x - near) <= 1e-12 * x ? near : ceil(x));
     }
     b.far = b.border[m - 1];
     return b;
