@@ -63,23 +63,56 @@ typedef __attribute__((address_space(3))) v4s lds_v4s;
 typedef __attribute__((address_space(3))) v4u lds_v4u;
 typedef __attribute__((address_space(3))) float lds_f32;
 
-// Which piece of the launch a workgroup takes.  Its `units` (sequences, or shares of their keys) have `per` pieces each: a unit's pieces
-// go to one XCD, where the rows of keys that several of them read are in its L2 and heads that lie side by side in memory are read at
-// the same time; neighbouring units, which are as long as each other where the batch is sorted by length, go to different XCDs
-// (workgroup ids go round the 8 XCDs).  The units left over when eight at a time have been dealt are spread over all XCDs.
-// DEAL_MEASURE
+// Which piece of the launch a workgroup takes.  Its `units` have `per` pieces each.  Workgroup ids go round the 8 XCDs: a unit's pieces go
+// to one of them, where the rows that several of them read are in its L2; neighbouring units, which are as long as each other where
+// the batch is sorted by length, go to different ones.  The units left over when eight at a time have been dealt are spread over all
+// XCDs.  Two ways:
+//   like pieces (no causal mask): a unit is a sequence, whose heads lie side by side in memory, and its pieces come one after the
+//   other (forward of 64 x 256 x 12 x 64 26 us; with a key head as the unit 33);
+//   pieces of which the first take longest (causal): a unit is a key head, and kMixed units are taken together, their first pieces
+//   first, so that what ends last is short (causal 2 x 4096 x 16 (4) x 128 unit after unit / this way: forward 216 / 170 us, dq 247 /
+//   226, dk and dv 459 / 364).
 struct Piece {
     uint32_t unit, rest;
 };
-__device__ __forceinline__ Piece deal_units(uint32_t blk, uint32_t units, uint32_t per)
+constexpr uint32_t kMixed = 4;
+__device__ __forceinline__ Piece deal_units(uint32_t blk, uint32_t units, uint32_t per, bool alike)
 {
-    const uint32_t even = units & ~7u;
-    if (blk < even * per) {
-        const uint32_t n = blk >> 3, u = n / per;
-        return {u * 8 + (blk & 7u), n - u * per};
+    const uint32_t mine = units >> 3, left = units & 7u;
+    if (blk < 8 * mine * per) {
+        const uint32_t n = blk >> 3, x = blk & 7u;
+        if (alike) {
+            const uint32_t u = n / per;
+            return {u * 8 + x, n - u * per};
+        }
+        const uint32_t turn = n / (kMixed * per), in = n - turn * kMixed * per;
+        const uint32_t m = turn * kMixed + kMixed > mine ? mine - turn * kMixed : kMixed, rest = in / m;
+        return {(turn * kMixed + in - rest * m) * 8 + x, rest};
     }
-    const uint32_t n = xcd_piece(blk - even * per, (units - even) * per), u = n / per;
-    return {even + u, n - u * per};
+    uint32_t n = blk - 8 * mine * per;
+    if (alike) {
+        n = xcd_piece(n, left * per);
+        const uint32_t u = n / per;
+        return {8 * mine + u, n - u * per};
+    }
+    const uint32_t rest = n / left;
+    return {8 * mine + n - rest * left, rest};
+}
+// The pieces of kernels that have `tiles` tiles for each of `each` things (heads, parts) of a key head: key head of the batch, number of
+// the thing, and tile.
+struct HeadPiece {
+    uint32_t head, which, tile;
+};
+__device__ __forceinline__ HeadPiece deal_heads(uint32_t blk, uint32_t batch, uint32_t kv_heads, uint32_t each, uint32_t tiles, bool alike)
+{
+    if (alike) {
+        const Piece p = deal_units(blk, batch, kv_heads * each * tiles, true);
+        const uint32_t n = p.rest / tiles, g = n / each;
+        return {p.unit * kv_heads + g, n - g * each, p.rest - n * tiles};
+    }
+    const Piece p = deal_units(blk, batch * kv_heads, each * tiles, false);
+    const uint32_t tile = p.rest / each;
+    return {p.unit, p.rest - tile * each, tile};
 }
 
 struct v8f {

@@ -27,9 +27,10 @@ __global__ __launch_bounds__(256, sizeof(T) * D == 512 ? 1 : 2) void attention_d
     constexpr int kKeys = dq_keys<T, D>(), kTileBytes = kKeys * tile::kRowBytes;
     const int tid = threadIdx.x, lane = tid & 63, half = lane >> 5, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const uint32_t tiles = (uint32_t)(a.q_len + kRowTile - 1) / kRowTile;
-    const Piece piece = deal_units(blockIdx.x, (uint32_t)a.batch, (uint32_t)(a.heads * a.q_parts) * tiles);
-    const uint32_t rt = tiles - 1 - piece.rest % tiles;                     // the longest rows of a causal head first
-    const int part = (int)(piece.rest / tiles % (uint32_t)a.q_parts), b = (int)piece.unit, h = (int)(piece.rest / tiles / (uint32_t)a.q_parts);
+    const HeadPiece piece = deal_heads(blockIdx.x, (uint32_t)a.batch, (uint32_t)a.kv_heads, (uint32_t)(a.group * a.q_parts), tiles, !a.causal);
+    const uint32_t rt = tiles - 1 - piece.tile;                             // the longest rows of a causal head first
+    const int part = (int)(piece.which % (uint32_t)a.q_parts), b = (int)(piece.head / (uint32_t)a.kv_heads);
+    const int h = (int)(piece.head % (uint32_t)a.kv_heads) * a.group + (int)(piece.which / (uint32_t)a.q_parts);
     const int q0 = (int)rt * kRowTile, bh = b * a.heads + h;
     const int nq = clamped(a.q_lens, b, a.q_len), nk = clamped(a.k_lens, b, a.k_len), shift = a.causal ? nk - nq : 0;
     const int rows = nq - q0 < kRowTile ? nq - q0 : kRowTile;
@@ -194,9 +195,15 @@ __global__ __launch_bounds__(256, sizeof(T) * D == 512 ? 1 : 2) void attention_d
         return;
     }
     const uint32_t tiles = (uint32_t)(a.k_len + kRowTile - 1) / kRowTile;
-    const Piece piece = deal_units(blockIdx.x - extra, (uint32_t)a.batch, (uint32_t)(a.kv_heads * a.kv_parts) * tiles);
-    const int part = (int)(piece.rest / tiles % (uint32_t)a.kv_parts), b = (int)piece.unit, hk = (int)(piece.rest / tiles / (uint32_t)a.kv_parts);
-    const int k0 = (int)(piece.rest % tiles) * kRowTile, bh = b * a.kv_heads + hk;
+    // (workgroups that read the same queries: a part of those of a key head)
+    Piece piece;
+    if (a.causal) piece = deal_units(blockIdx.x - extra, (uint32_t)(a.batch * a.kv_heads * a.kv_parts), tiles, false);
+    else {
+        const HeadPiece p = deal_heads(blockIdx.x - extra, (uint32_t)a.batch, (uint32_t)a.kv_heads, (uint32_t)a.kv_parts, tiles, true);
+        piece = {p.head * (uint32_t)a.kv_parts + p.which, p.tile};
+    }
+    const int part = (int)(piece.unit % (uint32_t)a.kv_parts), bh = (int)(piece.unit / (uint32_t)a.kv_parts);
+    const int k0 = (int)piece.rest * kRowTile, hk = bh % a.kv_heads, b = bh / a.kv_heads;
     const int nq = clamped(a.q_lens, b, a.q_len), nk = clamped(a.k_lens, b, a.k_len), shift = a.causal ? nk - nq : 0;
     // queries that see a key of the tile: from `first` on; the same for every head of the group
     int first = a.causal && k0 > shift ? (k0 - shift) / kQueries * kQueries : 0;

@@ -101,9 +101,10 @@ __global__ __launch_bounds__(256, sizeof(T) * D == 512 ? 1 : 2) void attention_f
     constexpr int kTileBytes = kKeyTile * tile::kRowBytes;
     const int tid = threadIdx.x, lane = tid & 63, half = lane >> 5, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const uint32_t tiles = (uint32_t)(a.q_len + kRowTile - 1) / kRowTile;
-    const Piece piece = deal_units(blockIdx.x, (uint32_t)a.batch, (uint32_t)a.heads * tiles);
+    const HeadPiece piece = deal_heads(blockIdx.x, (uint32_t)a.batch, (uint32_t)a.kv_heads, (uint32_t)a.group, tiles, !a.causal);
     // the longest rows of a causal head first
-    const int q0 = (int)(tiles - 1 - piece.rest % tiles) * kRowTile, h = (int)(piece.rest / tiles), b = (int)piece.unit;
+    const int q0 = (int)(tiles - 1 - piece.tile) * kRowTile, b = (int)(piece.head / (uint32_t)a.kv_heads);
+    const int h = (int)(piece.head % (uint32_t)a.kv_heads) * a.group + (int)piece.which;
     const int nq = clamped(a.q_lens, b, a.q_len), nk = clamped(a.k_lens, b, a.k_len), shift = a.causal ? nk - nq : 0;
     const int rows = nq - q0 < kRowTile ? nq - q0 : kRowTile;               // live rows of the tile (may be negative)
     int keys = rows > 0 ? nk : 0;
@@ -221,7 +222,7 @@ __global__ __launch_bounds__(256) void attention_few_kernel(AttnArgs a)
     __shared__ float stat[2][4][kFewRows];
     const int tid = threadIdx.x, lane = tid & 63, half = lane >> 5, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const uint32_t rows = (uint32_t)a.group * (uint32_t)a.q_len, tiles = (rows + kFewRows - 1) / kFewRows;
-    const Piece piece = deal_units(blockIdx.x, (uint32_t)(a.batch * a.splits), tiles * (uint32_t)a.kv_heads);
+    const Piece piece = deal_units(blockIdx.x, (uint32_t)(a.batch * a.splits), tiles * (uint32_t)a.kv_heads, true);
     const uint32_t split = piece.unit % (uint32_t)a.splits, rt = piece.rest / (uint32_t)a.kv_heads;
     const int g = (int)(piece.rest % (uint32_t)a.kv_heads), b = (int)(piece.unit / (uint32_t)a.splits);
     const int nq = clamped(a.q_lens, b, a.q_len), nk = clamped(a.k_lens, b, a.k_len), shift = a.causal ? nk - nq : 0;

@@ -79,7 +79,7 @@ __global__ __launch_bounds__(64 * WAVES, 2) void attention_one_pass_kernel(AttnA
     constexpr int kLanesPerRow = tile::kUnits, kRowsAtOnce = kThreads / kLanesPerRow, kRounds = kQueries / kRowsAtOnce;
     __shared__ float stat[2][2][kQueries];                                  // base-2 log-sum-exp and delta of a step's queries
     const int tid = threadIdx.x, lane = tid & 63, half = lane >> 5, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const Piece piece = deal_units(blockIdx.x, (uint32_t)a.batch, (uint32_t)a.kv_heads);
+    const Piece piece = deal_units(blockIdx.x, (uint32_t)a.batch, (uint32_t)a.kv_heads, true);
     const int hk = (int)piece.rest, b = (int)piece.unit;
     const int nq = clamped(a.q_lens, b, a.q_len), nk = clamped(a.k_lens, b, a.k_len), shift = a.causal ? nk - nq : 0;
     const int per_head = nk > 0 ? (nq + kQueries - 1) / kQueries : 0, steps = per_head * a.group;
