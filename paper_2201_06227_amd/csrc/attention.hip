@@ -125,7 +125,7 @@ bool one_pass(const egeria_attention_desc *d)
 struct Plan {
     bool one = false;
     size_t off_delta = 0, off_part = 0, off_o = 0, off_ml = 0, off_q = 0, off_kv = 0, total = 0;
-    int splits = 0, q_parts = 1, kv_parts = 1;
+    int splits = 0, q_parts = 1, kv_parts = 1, whole = 0;
 };
 Plan make_plan(const egeria_attention_desc *d, bool backward)
 {
@@ -134,7 +134,16 @@ Plan make_plan(const egeria_attention_desc *d, bool backward)
     take(256);
     if (backward && one_pass(d)) {
         p.one = true;
-        p.off_part = take((size_t)d->batch * d->heads * position_rows(d->bias) * 4);
+        // rounds of as many key heads as run at a time; what the last round would have fewer of is done in parts, so that it is short
+        const int64_t units = (int64_t)d->batch * d->kv_heads, slots = (int64_t)compute_units() * (d->k_len <= 128 ? 2 : 1);
+        const int64_t steps = ((int64_t)d->q_len + one_pass_queries(d->dtype) - 1) / one_pass_queries(d->dtype) * (d->heads / d->kv_heads);
+        const int64_t over = units % slots;
+        int64_t parts = over && units > slots ? slots / over : 1;
+        parts = parts > steps ? steps : parts;
+        p.kv_parts = (int)(parts < 1 ? 1 : (parts > 16 ? 16 : parts));
+        p.whole = (int)(p.kv_parts > 1 ? units - over : units);
+        p.off_part = take((size_t)d->batch * d->heads * p.kv_parts * position_rows(d->bias) * 4);
+        if (p.kv_parts > 1) p.off_kv = take((size_t)p.kv_parts * over * d->k_len * 64 * 8);
         return p;
     }
     if (backward) {
@@ -234,7 +243,8 @@ egeria_status egeria_attention_backward(const egeria_attention_desc *desc, const
     hipStream_t st = (hipStream_t)stream;
     bool vec = true;
     for (const egeria_heads *t : {dout, q, k, v, out, dq, dk, dv}) vec = vec && wide_rows(t, desc);
-    a.table_parts = (int64_t)a.batch * (p.one ? 1 : a.q_parts * row_tiles(desc));
+    a.whole = p.whole;
+    a.table_parts = (int64_t)a.batch * (p.one ? a.kv_parts : a.q_parts * row_tiles(desc));
     EG_HIP((p.one ? launch_attention_one_pass : launch_attention_backward)(a, (egeria_dtype)desc->dtype, vec, st));
     return EGERIA_OK;
 }

@@ -22,6 +22,7 @@ struct AttnArgs {
     int32_t table_rows;
     int32_t batch, heads, kv_heads, group, q_len, k_len, dim, causal;
     int32_t splits, q_parts, kv_parts;
+    int32_t whole;                          // one pass: key heads of the batch that are not done in (kv_parts) parts
     int64_t table_parts;                    // partial sums of each head in `partials`
     float scale;
     Buckets b;
@@ -42,7 +43,28 @@ hipError_t launch_attention_backward(const AttnArgs &a, egeria_dtype dt, bool ve
 constexpr int kOnePassKeys = 256;
 constexpr size_t kMostLds = 156 * 1024;
 size_t one_pass_lds(const egeria_attention_desc *d, bool table_grad);
+inline int one_pass_queries(int32_t dtype) { return dtype == EGERIA_F32 ? 32 : 64; }       // queries of a step
 hipError_t launch_attention_one_pass(const AttnArgs &a, egeria_dtype dt, bool vec, hipStream_t st);
+
+// Joins parts of sums: one of up to three tensors [batch, heads, len, ..] in each blockIdx.y.
+struct JoinJob {
+    View out;
+    const float *sum;                       // [parts][rows][stride]
+    int64_t rows;                           // of the heads from number `first` on
+    int32_t heads, len, parts, stride, first;
+};
+struct JoinJobs {
+    JoinJob job[3];
+    int n = 0;
+    int64_t most = 0;                       // rows
+    void add(const JoinJob &j)
+    {
+        if (j.parts < 2 || j.rows == 0) return;
+        job[n++] = j;
+        most = j.rows > most ? j.rows : most;
+    }
+};
+hipError_t launch_join_parts(const JoinJobs &jobs, int dim, egeria_dtype dt, bool vec, hipStream_t st);
 
 // a launcher's instance for the type, the head size and how the rows are read
 #define EG_PICK(go, a, dt, vec, st)                                                                              \

@@ -361,16 +361,7 @@ __global__ __launch_bounds__(256, sizeof(T) * D == 512 ? 1 : 2) void attention_d
     }
 }
 
-// Joins parts of sums: one of up to three tensors [batch, heads, len, D] in each blockIdx.y, a thread for four features of a row.
-struct JoinJob {
-    View out;
-    const float *sum;                       // [parts][batch * heads * len][stride]
-    int64_t rows;
-    int32_t heads, len, parts, stride;
-};
-struct JoinJobs {
-    JoinJob job[3];
-};
+// a thread for four features of a row
 template <typename T, int D, bool VEC>
 __global__ __launch_bounds__(256) void attention_join_parts_kernel(JoinJobs jobs, int dim)
 {
@@ -384,9 +375,18 @@ __global__ __launch_bounds__(256) void attention_join_parts_kernel(JoinJobs jobs
         const float4 x = *(const float4 *)(j.sum + ((int64_t)p * j.rows + row) * j.stride + f);
         s.x += x.x, s.y += x.y, s.z += x.z, s.w += x.w;
     }
-    const int i = (int)(row % j.len), h = (int)(row / j.len % j.heads), b = (int)(row / j.len / j.heads);
+    const int i = (int)(row % j.len), bh = j.first + (int)(row / j.len), h = bh % j.heads, b = bh / j.heads;
     T *out = (T *)j.out.p + ((int64_t)b * j.out.sb + (int64_t)i * j.out.st + (int64_t)h * j.out.sh);
     store4<T, VEC>(out, f, dim, s.x, s.y, s.z, s.w);
+}
+
+template <typename T, int D, bool VEC>
+hipError_t go_join(const JoinJobs &jobs, int dim, hipStream_t st)
+{
+    if (jobs.n == 0) return hipSuccess;
+    const int64_t per = 256 / (D / 4);
+    return launch_k(EGERIA_KERNEL_NONE, attention_join_parts_kernel<T, D, VEC>, dim3((unsigned)((jobs.most + per - 1) / per), (unsigned)jobs.n), dim3(256), 0,
+                    st, jobs, dim);
 }
 
 template <typename T, int D, bool VEC>
@@ -410,26 +410,21 @@ hipError_t go_backward(const AttnArgs &a, hipStream_t st)
         e = launch_k(EGERIA_KERNEL_ATTENTION, attention_dkv_kernel<T, D, VEC>, dim3((unsigned)k_blocks), dim3(256), lds, st, a);
         if (e != hipSuccess) return e;
     }
-    JoinJobs jobs = {};
-    int n = 0;
-    int64_t most = 0;
-    auto join = [&](const View &out, const float *sum, int heads, int len, int parts, int stride) {
-        const int64_t rows = (int64_t)a.batch * heads * len;
-        if (parts < 2 || rows == 0) return;
-        jobs.job[n++] = {out, sum, rows, heads, len, parts, stride};
-        most = rows > most ? rows : most;
-    };
-    join(a.dq, a.part_q, a.heads, a.q_len, a.q_parts, D);
-    join(a.dk, a.part_kv, a.kv_heads, a.k_len, a.kv_parts, 2 * D);
-    join(a.dv, a.part_kv + D, a.kv_heads, a.k_len, a.kv_parts, 2 * D);
-    if (n == 0) return hipSuccess;
-    const int64_t per = 256 / (D / 4);
-    return launch_k(EGERIA_KERNEL_NONE, attention_join_parts_kernel<T, D, VEC>, dim3((unsigned)((most + per - 1) / per), (unsigned)n), dim3(256), 0, st,
-                    jobs, (int)a.dim);
+    JoinJobs jobs;
+    const int64_t rows = (int64_t)a.batch * a.heads * a.q_len, keys = (int64_t)a.batch * a.kv_heads * a.k_len;
+    jobs.add({a.dq, a.part_q, rows, a.heads, a.q_len, a.q_parts, D, 0});
+    jobs.add({a.dk, a.part_kv, keys, a.kv_heads, a.k_len, a.kv_parts, 2 * D, 0});
+    jobs.add({a.dv, a.part_kv + D, keys, a.kv_heads, a.k_len, a.kv_parts, 2 * D, 0});
+    return go_join<T, D, VEC>(jobs, a.dim, st);
 }
 
 }  // namespace
 
+hipError_t launch_join_parts(const JoinJobs &jobs, int dim, egeria_dtype dt, bool vec, hipStream_t st)       // (heads of at most 64)
+{
+    if (dt == EGERIA_F32) return vec ? go_join<float, 64, true>(jobs, dim, st) : go_join<float, 64, false>(jobs, dim, st);
+    return vec ? go_join<uint16_t, 64, true>(jobs, dim, st) : go_join<uint16_t, 64, false>(jobs, dim, st);
+}
 hipError_t launch_attention_backward(const AttnArgs &a, egeria_dtype dt, bool vec, hipStream_t st) { return EG_PICK(go_backward, a, dt, vec, st); }
 
 }  // namespace egeria

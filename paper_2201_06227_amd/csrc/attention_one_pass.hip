@@ -79,10 +79,12 @@ __global__ __launch_bounds__(64 * WAVES, 2) void attention_one_pass_kernel(AttnA
     constexpr int kLanesPerRow = tile::kUnits, kRowsAtOnce = kThreads / kLanesPerRow, kRounds = kQueries / kRowsAtOnce;
     __shared__ float stat[2][2][kQueries];                                  // base-2 log-sum-exp and delta of a step's queries
     const int tid = threadIdx.x, lane = tid & 63, half = lane >> 5, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const Piece piece = deal_units(blockIdx.x, (uint32_t)a.batch, (uint32_t)a.kv_heads, true);
-    const int hk = (int)piece.rest, b = (int)piece.unit;
+    // the key heads that are left over when every compute unit has had the same number are done in parts
+    const int over = (int)blockIdx.x - a.whole, parts = over < 0 ? 1 : a.kv_parts, part = over < 0 ? 0 : over % parts;
+    const int bh = over < 0 ? (int)blockIdx.x : a.whole + over / parts, hk = bh % a.kv_heads, b = bh / a.kv_heads;
     const int nq = clamped(a.q_lens, b, a.q_len), nk = clamped(a.k_lens, b, a.k_len), shift = a.causal ? nk - nq : 0;
-    const int per_head = nk > 0 ? (nq + kQueries - 1) / kQueries : 0, steps = per_head * a.group;
+    const int per_head = nk > 0 ? (nq + kQueries - 1) / kQueries : 0, all = per_head * a.group;
+    const int begin = (int)((int64_t)all * part / parts), steps = (int)((int64_t)all * (part + 1) / parts);
     const int chunks = (nk + Across<T, 8>::kRows - 1) / Across<T, 8>::kRows;
 
     const uint32_t lds = (uint32_t)(uintptr_t)(lds_byte *)smem, lds_ds = lds + L::kKeyBytes, lds_q = lds_ds + L::kDsBytes;
@@ -101,7 +103,8 @@ __global__ __launch_bounds__(64 * WAVES, 2) void attention_one_pass_kernel(AttnA
     const char *q_base = qr.rows.base, *g_base = gr.rows.base, *o_base = orow.base;
     v4u next_g[kRounds], next_o[kRounds];
     float next_lse[kRounds];
-    int next_h = hk * a.group, next_i = 0;                                  // head and first query of the next step to be staged
+    int next_h = hk * a.group + (per_head > 0 ? begin / per_head : 0), next_i = (per_head > 0 ? begin % per_head : 0) * kQueries;                                  // head and first query of the next step to be staged
+    int now_h = next_h, now_i = next_i;                                     // of the step at hand
     auto stage = [&](uint32_t to) __attribute__((always_inline)) {
         const int h = next_h, i0 = next_i;
         next_i += kQueries;
@@ -144,7 +147,7 @@ __global__ __launch_bounds__(64 * WAVES, 2) void attention_one_pass_kernel(AttnA
     v16f dk[2], dv[2];
 #pragma unroll
     for (int n = 0; n < 2; ++n) dk[n] = dv[n] = v16f(0.0f);
-    if (steps > 0) {
+    if (begin < steps) {
         Feed<T, D, VEC, 32 * WAVES, kThreads> keys;
         keys.open(a.k, b, hk, nk, a.dim, tid);
         keys.load(lds, 0);
@@ -163,7 +166,8 @@ __global__ __launch_bounds__(64 * WAVES, 2) void attention_one_pass_kernel(AttnA
     const typename tile::Lane at = tile::lane_at(lds_q, lane);
     const uint32_t at_k = Across<T, tile::kUnits>::lane_at(lds, lane), at_ds = Across<T, 8>::lane_at(lds_ds, lane);
     float left = 0.0f, right = 0.0f;
-    int lut_head = -1, now_h = hk * a.group, now_i = 0;
+    int lut_head = -1;
+    auto table_sums = [&](int h, int q) { return a.partials + (((int64_t)h * a.batch + b) * a.kv_parts + q) * a.table_rows; };
     auto finish_head = [&](int h) {                                         // the sums by bucket of a head whose queries are done
         left = wave_sum(left);
         right = wave_sum(right);
@@ -171,7 +175,7 @@ __global__ __launch_bounds__(64 * WAVES, 2) void attention_one_pass_kernel(AttnA
             mine[0] += left;
             mine[entries - 1] += right;
         }
-        bucket_sums<kThreads>(bias.spans, sums, 2 * WAVES, entries, entries, a.table_rows, a.partials + ((int64_t)h * a.batch + b) * a.table_rows);
+        bucket_sums<kThreads>(bias.spans, sums, 2 * WAVES, entries, entries, a.table_rows, table_sums(h, part));
         left = right = 0.0f;
         __syncthreads();
     };
@@ -312,20 +316,24 @@ __global__ __launch_bounds__(64 * WAVES, 2) void attention_one_pass_kernel(AttnA
             }
         }
     };
-    for (int step = 0; step < steps; step += 2) {
+    for (int step = begin; step < steps; step += 2) {
         one_step(Const<0>(), step);
         if (step + 1 < steps) one_step(Const<1>(), step + 1);
     }
     if (a.partials) {
         __syncthreads();
-        if (steps > 0) finish_head(hk * a.group + a.group - 1);
-        else
-            for (int n = tid; n < a.group * a.table_rows; n += kThreads)
-                a.partials[((int64_t)(hk * a.group + n / a.table_rows) * a.batch + b) * a.table_rows + n % a.table_rows] = 0.0f;
+        if (begin < steps) finish_head(lut_head);
+        // heads and parts that have not been written
+        const int h0 = hk * a.group, seen0 = begin < steps ? h0 + begin / per_head : h0, seen1 = begin < steps ? lut_head + 1 : h0;
+        for (int n = tid; n < a.group * a.table_rows; n += kThreads) {
+            const int h = h0 + n / a.table_rows;
+            for (int q = part; q < a.kv_parts; q += parts)
+                if (q != part || h < seen0 || h >= seen1) table_sums(h, q)[n % a.table_rows] = 0.0f;
+        }
     }
     // queries behind the last step
     const int done = per_head * kQueries, rest = a.q_len - done;
-    for (int64_t n = tid; n < (int64_t)rest * a.group * (D / 4); n += kThreads) {
+    for (int64_t n = tid; part == 0 && n < (int64_t)rest * a.group * (D / 4); n += kThreads) {
         const int f = (int)(n % (D / 4)) * 4, h = hk * a.group + (int)(n / (D / 4) % a.group), i = done + (int)(n / (D / 4) / a.group);
         store4<T, VEC>((T *)a.dq.p + ((int64_t)b * a.dq.sb + (int64_t)i * a.dq.st + (int64_t)h * a.dq.sh), f, a.dim, 0.0f, 0.0f, 0.0f, 0.0f);
     }
@@ -334,9 +342,21 @@ __global__ __launch_bounds__(64 * WAVES, 2) void attention_one_pass_kernel(AttnA
 #pragma unroll
         for (int n = 0; n < 2; ++n) dk[n] = dv[n] = v16f(0.0f);
     }
-    const uint32_t room = lds + 32 * wave * tile::kRowBytes;
-    store_rows<T, D, VEC>(dk, a.scale, a.dk, b, hk, jw, a.k_len, a.dim, room, lane);
-    store_rows<T, D, VEC>(dv, 1.0f, a.dv, b, hk, jw, a.k_len, a.dim, room, lane);
+    if (parts == 1) {
+        const uint32_t room = lds + 32 * wave * tile::kRowBytes;
+        store_rows<T, D, VEC>(dk, a.scale, a.dk, b, hk, jw, a.k_len, a.dim, room, lane);
+        store_rows<T, D, VEC>(dv, 1.0f, a.dv, b, hk, jw, a.k_len, a.dim, room, lane);
+    } else if (j < a.k_len) {
+        float *sum = a.part_kv + (((int64_t)part * (a.batch * a.kv_heads - a.whole) + (bh - a.whole)) * a.k_len + j) * (2 * D);
+#pragma unroll
+        for (int n = 0; n < 2; ++n)
+#pragma unroll
+            for (int r = 0; r < 16; r += 4) {
+                const int f = 32 * n + row_of(r, half);
+                *(float4 *)(sum + f) = make_float4(dk[n][r] * a.scale, dk[n][r + 1] * a.scale, dk[n][r + 2] * a.scale, dk[n][r + 3] * a.scale);
+                *(float4 *)(sum + D + f) = make_float4(dv[n][r], dv[n][r + 1], dv[n][r + 2], dv[n][r + 3]);
+            }
+    }
 }
 
 template <typename T, int WAVES>
@@ -354,8 +374,14 @@ hipError_t go_one_pass(const AttnArgs &a, hipStream_t st)
     const size_t lds = lds_of<T, WAVES>(a.table ? &a.b : nullptr, a.partials != nullptr);
     hipError_t e = allow_lds(attention_one_pass_kernel<T, VEC, WAVES>, lds, done);
     if (e != hipSuccess) return e;
-    e = launch_k(EGERIA_KERNEL_ATTENTION, attention_one_pass_kernel<T, VEC, WAVES>, dim3((unsigned)((int64_t)a.batch * a.kv_heads)), dim3(64 * WAVES), lds,
+    const int64_t over = (int64_t)a.batch * a.kv_heads - a.whole;
+    e = launch_k(EGERIA_KERNEL_ATTENTION, attention_one_pass_kernel<T, VEC, WAVES>, dim3((unsigned)(a.whole + over * a.kv_parts)), dim3(64 * WAVES), lds,
                  st, a);
+    if (e != hipSuccess) return e;
+    JoinJobs jobs;
+    jobs.add({a.dk, a.part_kv, over * a.k_len, a.kv_heads, a.k_len, a.kv_parts, 128, a.whole});
+    jobs.add({a.dv, a.part_kv + 64, over * a.k_len, a.kv_heads, a.k_len, a.kv_parts, 128, a.whole});
+    e = launch_join_parts(jobs, a.dim, sizeof(T) == 4 ? EGERIA_F32 : EGERIA_BF16, VEC, st);
     if (e != hipSuccess || !a.dtable) return e;
     return launch_table_reduce(a.partials, a.heads, a.table_parts, a.table_rows, a.dtable, st);
 }

@@ -273,7 +273,8 @@ def test_attention_lengths(eg, dtype, causal, with_bias):
     ((64, 40, 33, 2, 2, 64), False, None, False), ((32, 70, 130, 8, 4, 40), True, None, True), ((43, 130, 200, 3, 3, 64), False, (32, 128, True), True),
     ((130, 5, 256, 1, 1, 33), False, (16, 40, True), False), ((16, 100, 128, 16, 8, 64), True, (32, 128, False), True), ((128, 1, 1, 1, 1, 1), False, None, False),
     ((64, 64, 255, 2, 2, 16), True, (8, 20, True), True), ((32, 300, 64, 4, 4, 48), True, (32, 100, False), True), ((26, 200, 256, 10, 5, 64), False, (20, 50, True), True),
-    ((64, 33, 100, 2, 2, 64), False, (4, 1024, True), False)], ids=str)
+    ((64, 33, 100, 2, 2, 64), False, (4, 1024, True), False), ((65, 100, 130, 8, 4, 32), True, (16, 40, False), True), ((130, 70, 40, 4, 4, 16), False, (16, 40, True), False),
+    ((129, 200, 33, 4, 4, 40), True, None, True)], ids=str)
 def test_attention_many_short_sequences(eg, dtype, shape, causal, bias, lens):
     """Batches with a workgroup for each key head: few keys, queries of every number, shared key heads, empty sequences."""
     b, nq, nk, h = shape[:4]
