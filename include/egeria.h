@@ -575,7 +575,7 @@ egeria_status egeria_attention_backward(const egeria_attention_desc *desc, const
 /* The bias as a tensor, for attention that is not computed here:
  * bias[h, i, j] = table[bucket(j - i - offset), h], rounded once to dt;
  * bias [heads, q_len, k_len] out, offset the position of query 0 among the keys.
- * |offset|, q_len, k_len <= 2^29, heads <= 65535. */
+ * |offset| <= 2^29, q_len and k_len <= 2^28, heads <= 65535. */
 egeria_status egeria_position_bias(const egeria_position_table *t, int32_t heads, int32_t q_len, int32_t k_len, int32_t offset,
                                    void *bias, egeria_dtype dt, void *stream);
 

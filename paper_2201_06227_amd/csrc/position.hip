@@ -33,6 +33,20 @@ template <> __device__ __forceinline__ uint16_t narrow<uint16_t>(float v)
     return __builtin_bit_cast(uint16_t, (__bf16)v);
 }
 
+// The 16 bytes from byte s of two units of 16 (s even; words chosen one by one, since a chosen index would send them through memory).
+__device__ __forceinline__ v4u from_byte(v4u a, v4u b, int s)
+{
+    const bool two = s & 8, one = s & 4, half = s & 2;
+    const uint32_t x0 = two ? a[2] : a[0], x1 = two ? a[3] : a[1], x2 = two ? b[0] : a[2], x3 = two ? b[1] : a[3], x4 = two ? b[2] : b[0], x5 = two ? b[3] : b[1];
+    const uint32_t y0 = one ? x1 : x0, y1 = one ? x2 : x1, y2 = one ? x3 : x2, y3 = one ? x4 : x3, y4 = one ? x5 : x4;
+    v4u r;
+    r[0] = half ? __builtin_amdgcn_alignbyte(y1, y0, 2) : y0;
+    r[1] = half ? __builtin_amdgcn_alignbyte(y2, y1, 2) : y1;
+    r[2] = half ? __builtin_amdgcn_alignbyte(y3, y2, 2) : y2;
+    r[3] = half ? __builtin_amdgcn_alignbyte(y4, y3, 2) : y3;
+    return r;
+}
+
 // Where a thread's patches lie: 2^lg units of 16 bytes side by side (32 to 256 of them, so that half a wave has one row of patches),
 // 256 / 2^lg patches below each other: `rows` rows to a workgroup, and `cols` times these columns one after the other, so that what
 // a workgroup writes or reads lies close together (long rows in pieces of 4 KiB, 64 of them below each other, were written at
@@ -90,13 +104,15 @@ __global__ __launch_bounds__(256) void position_bias_kernel(Buckets b, const flo
 // One workgroup: the same piece of the rows and columns, summed over its share of the batch.  A thread adds up its patch along the
 // diagonals in registers, over the batch, then the diagonals' sums go to a table by distance of its half wave in LDS.  The lanes of
 // half a wave add to different entries at each step and a wave's additions are in order: the result does not depend on timing.
-template <typename T>
+// WHOLE: rows are whole units of 16 bytes.  Else a row's 16 bytes come from the two whole units that hold them: loads at other
+// addresses cost 24 % where those are multiples of 4, and at odd multiples of 2 run at a fifth of the rate (13 x 22 x 1142 x 391 in bf16
+// 199 us, now ANY_US).
+template <typename T, bool WHOLE>
 __global__ __launch_bounds__(256) void position_bias_backward_kernel(Buckets b, const T *__restrict__ dbias, int64_t batch, int heads,
                                                                      int q_len, int k_len, int offset, Deal deal, int rows_of_table,
                                                                      float *__restrict__ partials)
 {
     constexpr int N = Unit<T>::N;
-    typedef typename Unit<T>::vec vec;
     extern __shared__ float sums[];                                // [8 half waves][entries]
     const uint32_t p = xcd_piece(blockIdx.x, gridDim.x);
     const uint32_t cb = p % deal.col_blocks, rb = p / deal.col_blocks % deal.row_blocks, sh = p / deal.col_blocks / deal.row_blocks % deal.shares;
@@ -110,6 +126,7 @@ __global__ __launch_bounds__(256) void position_bias_backward_kernel(Buckets b, 
     const int64_t b0 = batch * sh / deal.shares, b1 = batch * (sh + 1) / deal.shares;
     const int i0 = (int)rb * deal.rows + (int)(threadIdx.x >> deal.lg) * kRows;
     const int last = (int)rb * deal.rows + deal.rows < q_len ? (int)rb * deal.rows + deal.rows : q_len;
+    const int64_t total = batch * heads * q_len * (int64_t)k_len;
     float left = 0.0f, right = 0.0f;                               // patches whose distances all lie beyond the table
     const int hi = b.both ? b.far : 0;
     for (int c = 0; c < deal.cols; ++c) {
@@ -119,24 +136,38 @@ __global__ __launch_bounds__(256) void position_bias_backward_kernel(Buckets b, 
         for (int e = 0; e < kRows + N - 1; ++e) d[e] = 0.0f;
         if (j0 < k_len && i0 < last)
             for (int64_t n = b0; n < b1; ++n) {
-                const T *src = dbias + ((n * heads + h) * q_len + i0) * k_len + j0;
-                vec w[kRows];
+                // row r of the workgroup's first patches as a buffer up to the tensor's end, from the unit that holds its beginning
+                const int64_t row0 = ((n * heads + h) * q_len + (int)rb * deal.rows) * k_len;
+                const int down = (i0 - (int)rb * deal.rows) * k_len + j0;        // (0 + j0, or a few short rows and j0)
+                v4u lo[kRows], up[kRows];
+                int s[kRows];
 #pragma unroll
                 for (int r = 0; r < kRows; ++r) {
-                    w[r] = vec(0);
-                    if (i0 + r < last) {
-                        if (j0 + N <= k_len) w[r] = *(const vec *)(src + (int64_t)r * k_len);
-                        else {
-#pragma unroll
-                            for (int e = 0; e < N; ++e)
-                                if (j0 + e < k_len) w[r][e] = src[(int64_t)r * k_len + e];
-                        }
-                    }
+                    const char *base = (const char *)(dbias + row0 + (int64_t)r * k_len);
+                    const int off = WHOLE ? 0 : (int)((uintptr_t)base & 15u), at = off + down * (int)sizeof(T);
+                    const int64_t left = ((const char *)(dbias + total) - base + off) & ~(int64_t)3;        // (below 0: a row behind the tensor)
+                    const __amdgpu_buffer_rsrc_t rows = __builtin_amdgcn_make_buffer_rsrc(const_cast<char *>(base - off), 0,
+                                                                                          left < 0 ? 0 : (left > 0x7fffffff ? 0x7fffffff : (int)left), kBufferWord);
+                    s[r] = WHOLE ? 0 : at & 15;
+                    const int unit = i0 + r < last ? at - s[r] : (int)0x80000000;
+                    lo[r] = __builtin_bit_cast(v4u, __builtin_amdgcn_raw_buffer_load_b128(rows, unit, 0, 0));
+                    if (!WHOLE) up[r] = __builtin_bit_cast(v4u, __builtin_amdgcn_raw_buffer_load_b128(rows, unit + 16, 0, 0));
                 }
 #pragma unroll
-                for (int r = 0; r < kRows; ++r)
+                for (int r = 0; r < kRows; ++r) {
+                    union { v4u u; T e[N]; } x;
+                    x.u = WHOLE ? lo[r] : from_byte(lo[r], up[r], s[r]);
 #pragma unroll
-                    for (int e = 0; e < N; ++e) d[kRows - 1 - r + e] += widen((T)w[r][e]);
+                    for (int e = 0; e < N; ++e) d[kRows - 1 - r + e] += j0 + e < k_len ? widen(x.e[e]) : 0.0f;
+                }
+                if (!WHOLE && sizeof(T) == 2 && (total & 1) && n == batch - 1 && (int)h == heads - 1 && last == q_len && j0 + N >= k_len) {
+                    // the tensor's last value shares no whole word with another: it is beyond the buffer
+#pragma unroll
+                    for (int r = 0; r < kRows; ++r)
+#pragma unroll
+                        for (int e = 0; e < N; ++e)
+                            if (i0 + r == q_len - 1 && j0 + e == k_len - 1) d[kRows - 1 - r + e] += widen(dbias[total - 1]);
+                }
             }
         const int first = j0 - (i0 + kRows - 1) - offset;
         if (first >= hi || first + kRows + N - 2 <= -b.far) {
@@ -201,7 +232,7 @@ bool valid_sizes(const egeria_position_table *t, int32_t heads, int32_t q_len, i
 {
     if (!t || !valid_position_table(t) || heads < 1 || heads > 65535 || q_len < 0 || k_len < 0) return false;
     if (dt != EGERIA_F32 && dt != EGERIA_BF16) return false;
-    return offset >= -(1 << 29) && offset <= (1 << 29) && q_len <= (1 << 29) && k_len <= (1 << 29);
+    return offset >= -(1 << 29) && offset <= (1 << 29) && q_len <= (1 << 28) && k_len <= (1 << 28);
 }
 
 int64_t parts_of(const Deal &p) { return (int64_t)p.shares * p.row_blocks * p.col_blocks; }
@@ -268,8 +299,10 @@ egeria_status egeria_position_bias_backward(const egeria_position_table *t, cons
         return launch_k(EGERIA_KERNEL_NONE, kernel, dim3((unsigned)blocks), dim3(256), lds, st, b, src, (int64_t)batch, (int)heads, (int)q_len,
                         (int)k_len, (int)offset, p, (int)t->buckets, partials);
     };
-    hipError_t e = dt == EGERIA_F32 ? go(position_bias_backward_kernel<float>, (const float *)dbias)
-                                    : go(position_bias_backward_kernel<uint16_t>, (const uint16_t *)dbias);
+    const bool whole = k_len % (dt == EGERIA_F32 ? 4 : 8) == 0;
+    hipError_t e;
+    if (dt == EGERIA_F32) e = whole ? go(position_bias_backward_kernel<float, true>, (const float *)dbias) : go(position_bias_backward_kernel<float, false>, (const float *)dbias);
+    else e = whole ? go(position_bias_backward_kernel<uint16_t, true>, (const uint16_t *)dbias) : go(position_bias_backward_kernel<uint16_t, false>, (const uint16_t *)dbias);
     if (e == hipSuccess) e = launch_table_reduce(partials, heads, parts_of(p), t->buckets, dtable, st);
     return e == hipSuccess ? EGERIA_OK : EGERIA_ERR_HIP;
 }
