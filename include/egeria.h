@@ -498,8 +498,9 @@ egeria_status egeria_cache_get(const egeria_cache_desc *desc, const void *cache,
  *   L_i  = log sum_j exp(s_ij),  p_ij = exp(s_ij - L_i),  o_i = sum_j p_ij v_j.
  * A row without a visible pair (an empty sequence, a query beyond n_q, a causal
  * query before the first key) has o = 0 and L = -infinity.  Keys and values at
- * or beyond n_k, and queries at or beyond n_q, are not read; a non-finite value
- * of a visible key may reach every query of its sequence, as in any product.
+ * or beyond n_k, and queries at or beyond n_q, may hold anything; a non-finite
+ * value of a key below n_k may reach every query of its sequence, as in any
+ * product.
  * Backward, from dout = dLoss/do:
  *   D_i = <dout_i, o_i>,  ds_ij = p_ij (<dout_i, v_j> - D_i)
  *   dq_i = scale sum_j ds_ij k_j,  dk_j = scale sum_{i, h of group g} ds_ij q_i,

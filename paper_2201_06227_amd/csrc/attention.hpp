@@ -279,6 +279,9 @@ struct Tile {
 // VEC: rows start on 16 bytes, hold a whole number of 16-byte units, do not overlap, and kRowTile of them span less than 2 GiB:
 // 16-byte loads, into tiles as buffer loads straight into LDS.  A unit beyond the row's end or of a token at or beyond `tokens` is asked
 // for beyond the buffer and arrives as zeros.  Otherwise: element by element.
+template <int ALIGN> struct AnyUnit;
+template <> struct AnyUnit<2> { typedef uint32_t type __attribute__((ext_vector_type(4), aligned(2))); };
+template <> struct AnyUnit<4> { typedef uint32_t type __attribute__((ext_vector_type(4), aligned(4))); };
 template <typename T, int D, bool VEC>
 struct Rows {
     const char *base;
@@ -292,22 +295,34 @@ struct Rows {
         tokens = n;
         dim = d;
     }
-    // 16 bytes: unit u of token t
+    // 16 bytes: unit u of token t, zeros beyond the row and the tokens.  The load itself is unconditional, from a place that exists (the
+    // tensor is not empty): under a condition each would be awaited before the next is asked for.
     __device__ __forceinline__ v4u unit(int t, int u) const
     {
         constexpr int N = 16 / (int)sizeof(T);
-        union { v4u w; T e[N]; } x;
-        x.w = v4u(0);
-        if (t < tokens && u * N < dim) {
-            const char *p = base + (int64_t)t * row_bytes + u * 16;
-            if constexpr (VEC) x.w = *(const v4u *)p;
-            else {
+        const bool ok = t < tokens && u * N < dim;
+        const int row = t < tokens ? t : (tokens > 0 ? tokens - 1 : 0);
+        const char *p = base + (int64_t)row * row_bytes;
+        v4u w;
+        if constexpr (VEC) w = *(const v4u *)(p + (u * N < dim ? u * 16 : 0));
+        else if (dim >= N) {
+            // at any address; a unit that the row ends in: the row's last 16 bytes, moved down
+            const int at = u * N <= dim - N ? u * N : dim - N, over = (u * N - at) * (int)sizeof(T);
+            w = *(const typename AnyUnit<sizeof(T)>::type *)(p + at * (int)sizeof(T));
+            w = from_byte(w, v4u(0), over < 16 ? over : 0);
+        } else {
+            union { v4u w; T e[N]; } x;
+            x.w = v4u(0);
 #pragma unroll
-                for (int e = 0; e < N; ++e)
-                    if (u * N + e < dim) x.e[e] = ((const T *)p)[e];
+            for (int e = 0; e < N; ++e) {
+                const T v = ((const T *)p)[e < dim ? e : 0];
+                x.e[e] = e < dim ? v : (T)0;
             }
+            w = x.w;
         }
-        return x.w;
+#pragma unroll
+        for (int k = 0; k < 4; ++k) w[k] = ok ? w[k] : 0u;
+        return w;
     }
     // fragment of the 32 tokens from t0 on, values 16 kk ...
     __device__ __forceinline__ typename FragOf<T>::type frag(int t0, int kk, int lane) const

@@ -33,20 +33,6 @@ template <> __device__ __forceinline__ uint16_t narrow<uint16_t>(float v)
     return __builtin_bit_cast(uint16_t, (__bf16)v);
 }
 
-// The 16 bytes from byte s of two units of 16 (s even; words chosen one by one, since a chosen index would send them through memory).
-__device__ __forceinline__ v4u from_byte(v4u a, v4u b, int s)
-{
-    const bool two = s & 8, one = s & 4, half = s & 2;
-    const uint32_t x0 = two ? a[2] : a[0], x1 = two ? a[3] : a[1], x2 = two ? b[0] : a[2], x3 = two ? b[1] : a[3], x4 = two ? b[2] : b[0], x5 = two ? b[3] : b[1];
-    const uint32_t y0 = one ? x1 : x0, y1 = one ? x2 : x1, y2 = one ? x3 : x2, y3 = one ? x4 : x3, y4 = one ? x5 : x4;
-    v4u r;
-    r[0] = half ? __builtin_amdgcn_alignbyte(y1, y0, 2) : y0;
-    r[1] = half ? __builtin_amdgcn_alignbyte(y2, y1, 2) : y1;
-    r[2] = half ? __builtin_amdgcn_alignbyte(y3, y2, 2) : y2;
-    r[3] = half ? __builtin_amdgcn_alignbyte(y4, y3, 2) : y3;
-    return r;
-}
-
 // Where a thread's patches lie: 2^lg units of 16 bytes side by side (32 to 256 of them, so that half a wave has one row of patches),
 // 256 / 2^lg patches below each other: `rows` rows to a workgroup, and `cols` times these columns one after the other, so that what
 // a workgroup writes or reads lies close together (long rows in pieces of 4 KiB, 64 of them below each other, were written at
