@@ -777,7 +777,7 @@ def _attention_desc(q, k, v, causal, scale, q_lens, k_lens, bias):
     if scale is None:
         scale = 1.0 / math.sqrt(dim) if dim else 0.0
     sizes = (_dt(q), batch, heads, ks[2], q_len, ks[1], dim, 1 if causal else 0)
-    return _desc_struct.pack(*sizes, scale, _lens(q_lens, batch), _lens(k_lens, batch), at), (*sizes[:7], rows), tab
+    return _desc_struct.pack(*sizes, scale, _lens(q_lens, batch), _lens(k_lens, batch), at), (*sizes, rows, bias and bias[1:]), tab
 
 
 _attention_ws = {}

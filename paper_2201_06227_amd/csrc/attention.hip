@@ -92,25 +92,28 @@ int64_t few_tiles(const egeria_attention_desc *d)
 
 // The forward kernel for few rows, and how many workgroups share a row tile's keys there (0: the other kernel).  A tile of 128 queries
 // leaves most of its waves without rows up to 32 queries; and where the tiles are few and the keys many, the keys have to be shared
-// to occupy the device.  Splits: up to two workgroups for each compute unit, of at least 256 keys.
+// to occupy the device.  Splits have at least 256 keys.
 int few_splits(const egeria_attention_desc *d)
 {
     const int64_t blocks = (int64_t)d->batch * d->heads * (((int64_t)d->q_len + kRowTile - 1) / kRowTile);
     const int64_t tiles = few_tiles(d);
-    if (d->q_len > 32 && !(blocks < 64 && d->k_len >= 1024)) return 0;
+    if (d->q_len > 32 && blocks >= 64) return 0;
     if (tiles == 0) return 0;
-    int64_t n = (512 + tiles - 1) / tiles;
+    // a round of workgroups, if their keys are few; else two, since the sequences' lengths may differ
+    const int64_t slots = (int64_t)compute_units() * (d->dtype == EGERIA_BF16 && d->head_dim <= 64 ? 2 : 1);
+    int64_t n = slots / tiles;
+    if (n < 1 || d->k_len / n > 1024) n = (2 * slots + tiles - 1) / tiles;
     const int64_t most = ((int64_t)d->k_len + 255) / 256;
     n = n > most ? most : n;
     return n < 1 ? 1 : (int)n;
 }
 
 // Parts that the steps of a backward kernel's workgroups are dealt in where there are few of them, each a sum in fp32 that a last
-// launch adds up: enough for `want` workgroups, of two steps at least, at most 16.
-int parts_of(int64_t blocks, int64_t steps, int64_t want)
+// launch adds up: as many as `slots` workgroups make, of two steps at least, at most 16.
+int parts_of(int64_t blocks, int64_t steps, int64_t slots)
 {
-    if (blocks == 0 || blocks * 2 > want) return 1;
-    int64_t n = (want + blocks - 1) / blocks;
+    if (blocks == 0) return 1;
+    int64_t n = slots / blocks;
     n = n > steps / 2 ? steps / 2 : n;
     return n < 1 ? 1 : (n > 16 ? 16 : (int)n);
 }
@@ -143,14 +146,15 @@ Plan make_plan(const egeria_attention_desc *d, bool backward)
         p.kv_parts = (int)(parts < 1 ? 1 : (parts > 16 ? 16 : parts));
         p.whole = (int)(p.kv_parts > 1 ? units - over : units);
         p.off_part = take((size_t)d->batch * d->heads * p.kv_parts * position_rows(d->bias) * 4);
-        if (p.kv_parts > 1) p.off_kv = take((size_t)p.kv_parts * over * d->k_len * 64 * 8);
+        if (p.kv_parts > 1) p.off_kv = take((size_t)p.kv_parts * over * d->k_len * padded_dim(d->head_dim) * 8);
         return p;
     }
     if (backward) {
         p.off_delta = take((size_t)d->batch * d->heads * d->q_len * 4);
-        const int64_t key_tiles = ((int64_t)d->k_len + kRowTile - 1) / kRowTile, wide = d->head_dim <= 64 ? 64 : 128;
-        p.q_parts = parts_of((int64_t)d->batch * d->heads * row_tiles(d), key_tiles * kRowTile / kKeyTile, 512);
-        p.kv_parts = parts_of((int64_t)d->batch * d->kv_heads * key_tiles, row_tiles(d) * kRowTile / kKeyTile * (d->heads / d->kv_heads), 1024);
+        const int64_t key_tiles = ((int64_t)d->k_len + kRowTile - 1) / kRowTile, wide = padded_dim(d->head_dim);
+        p.q_parts = parts_of((int64_t)d->batch * d->heads * row_tiles(d), key_tiles * kRowTile / kKeyTile, 2 * (int64_t)compute_units());
+        p.kv_parts = parts_of((int64_t)d->batch * d->kv_heads * key_tiles, row_tiles(d) * kRowTile / kKeyTile * (d->heads / d->kv_heads),
+                              (d->causal ? 4 : 2) * (int64_t)compute_units());         // (causal: pieces of unlike length, two rounds)
         p.off_part = take((size_t)d->batch * d->heads * row_tiles(d) * p.q_parts * position_rows(d->bias) * 4);
         if (p.q_parts > 1) p.off_q = take((size_t)p.q_parts * d->batch * d->heads * d->q_len * wide * 4);
         if (p.kv_parts > 1) p.off_kv = take((size_t)p.kv_parts * d->batch * d->kv_heads * d->k_len * wide * 8);
@@ -159,7 +163,7 @@ Plan make_plan(const egeria_attention_desc *d, bool backward)
     p.splits = few_splits(d);
     if (p.splits > 1) {
         const size_t rows = (size_t)few_tiles(d) * kFewRows * p.splits;
-        p.off_o = take(rows * (d->head_dim <= 64 ? 64 : 128) * 4);
+        p.off_o = take(rows * padded_dim(d->head_dim) * 4);
         p.off_ml = take(rows * 8);
     }
     return p;

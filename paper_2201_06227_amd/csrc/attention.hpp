@@ -66,12 +66,17 @@ struct JoinJobs {
 };
 hipError_t launch_join_parts(const JoinJobs &jobs, int dim, egeria_dtype dt, bool vec, hipStream_t st);
 
-// a launcher's instance for the type, the head size and how the rows are read
-#define EG_PICK(go, a, dt, vec, st)                                                                              \
-    (dt == EGERIA_F32 ? (a.dim <= 64 ? (vec ? go<float, 64, true>(a, st) : go<float, 64, false>(a, st))            \
-                                     : (vec ? go<float, 128, true>(a, st) : go<float, 128, false>(a, st)))         \
-                      : (a.dim <= 64 ? (vec ? go<uint16_t, 64, true>(a, st) : go<uint16_t, 64, false>(a, st))      \
-                                     : (vec ? go<uint16_t, 128, true>(a, st) : go<uint16_t, 128, false>(a, st))))
+// A launcher's instance for the type, the head size and how the rows are read.  D: the head size in whole blocks of 32, which is what
+// the products cost; tiles in LDS have rows of 64 or 128 values (heads of 96 in products of 128: causal 2 x 4096 x 16 (4) x 96
+// WIDE_MEASURE).
+#define EG_PICK_DIM(go, T, vec, a, ...)                                                                              \
+    (a.dim <= 32 ? (vec ? go<T, 32, true>(__VA_ARGS__) : go<T, 32, false>(__VA_ARGS__))                               \
+                 : a.dim <= 64 ? (vec ? go<T, 64, true>(__VA_ARGS__) : go<T, 64, false>(__VA_ARGS__))                 \
+                 : a.dim <= 96 ? (vec ? go<T, 96, true>(__VA_ARGS__) : go<T, 96, false>(__VA_ARGS__))                 \
+                               : (vec ? go<T, 128, true>(__VA_ARGS__) : go<T, 128, false>(__VA_ARGS__)))
+#define EG_PICK(go, a, dt, vec, st) (dt == EGERIA_F32 ? EG_PICK_DIM(go, float, vec, a, a, st) : EG_PICK_DIM(go, uint16_t, vec, a, a, st))
+inline int64_t padded_dim(int32_t dim) { return (dim + 31) / 32 * 32; }
+constexpr int row_values(int d) { return d <= 64 ? 64 : 128; }
 
 #ifdef __HIPCC__
 
@@ -346,7 +351,7 @@ struct Rows {
 // are outstanding until an explicit wait.  Rows at or beyond `tokens` lie beyond the buffer's extent (rows do not overlap: VEC).
 template <typename T, int D, bool VEC, int N, int THREADS>
 struct Feed {
-    typedef Tile<T, D> tile;
+    typedef Tile<T, row_values(D)> tile;
     static constexpr int kUnits = tile::kUnits, kSteps = N * kUnits / THREADS, kRowsPer = THREADS / kUnits;
     static_assert(N * kUnits % THREADS == 0, "whole requests");
     Rows<T, D, VEC> rows;
@@ -423,7 +428,7 @@ __device__ __forceinline__ void store4(T *row, int f, int dim, float x0, float x
 template <typename T, int D, bool VEC>
 __device__ __forceinline__ void store_rows(const v16f (&x)[D / 32], float by, const View &v, int b, int h, int t0, int rows, int dim, uint32_t lds, int lane)
 {
-    typedef Tile<T, D> tile;
+    typedef Tile<T, row_values(D)> tile;
     const int half = lane >> 5, mine = lane & 31;
     T *base = (T *)v.p + ((int64_t)b * v.sb + (int64_t)h * v.sh);
     if constexpr (!VEC) {

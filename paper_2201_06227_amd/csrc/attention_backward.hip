@@ -15,15 +15,15 @@ namespace {
 
 // Keys of a step of the dq kernel: half as many where a step would leave no LDS for the sums by distance.
 template <typename T, int D>
-constexpr int dq_keys() { return sizeof(T) * D == 512 ? kKeyTile / 2 : kKeyTile; }
+constexpr int dq_keys() { return sizeof(T) * row_values(D) == 512 ? kKeyTile / 2 : kKeyTile; }
 
 // ---- dq ---------------------------------------------------------------------------------------------------------
 
 template <typename T, int D, bool VEC>
-__global__ __launch_bounds__(256, sizeof(T) * D == 512 ? 1 : 2) void attention_dq_kernel(AttnArgs a)
+__global__ __launch_bounds__(256, sizeof(T) * row_values(D) == 512 ? 1 : 2) void attention_dq_kernel(AttnArgs a)
 {
     extern __shared__ __attribute__((aligned(16))) char smem[];
-    typedef Tile<T, D> tile;
+    typedef Tile<T, row_values(D)> tile;
     constexpr int kKeys = dq_keys<T, D>(), kTileBytes = kKeys * tile::kRowBytes;
     const int tid = threadIdx.x, lane = tid & 63, half = lane >> 5, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const uint32_t tiles = (uint32_t)(a.q_len + kRowTile - 1) / kRowTile;
@@ -180,10 +180,10 @@ constexpr int dkv_queries() { return D > 64 ? 32 : kKeyTile; }
 // ---- dk, dv -------------------------------------------------------------------------------------------------------
 
 template <typename T, int D, bool VEC>
-__global__ __launch_bounds__(256, sizeof(T) * D == 512 ? 1 : 2) void attention_dkv_kernel(AttnArgs a)
+__global__ __launch_bounds__(256, sizeof(T) * row_values(D) == 512 ? 1 : 2) void attention_dkv_kernel(AttnArgs a)
 {
     extern __shared__ __attribute__((aligned(16))) char smem[];
-    typedef Tile<T, D> tile;
+    typedef Tile<T, row_values(D)> tile;
     constexpr int kQueries = dkv_queries<D>(), kTileBytes = kQueries * tile::kRowBytes;
     constexpr bool kValuesInLds = D > 64;
     __shared__ float stat[2][2][kQueries];                                  // base-2 log-sum-exp and delta of a step's queries
@@ -369,7 +369,7 @@ __global__ __launch_bounds__(256) void attention_join_parts_kernel(JoinJobs jobs
     constexpr int kPer = 256 / (D / 4);
     const int f = threadIdx.x % (D / 4) * 4;
     const int64_t row = (int64_t)blockIdx.x * kPer + threadIdx.x / (D / 4);
-    if (row >= j.rows) return;
+    if (threadIdx.x >= kPer * (D / 4) || row >= j.rows) return;
     float4 s = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
     for (int p = 0; p < j.parts; ++p) {
         const float4 x = *(const float4 *)(j.sum + ((int64_t)p * j.rows + row) * j.stride + f);
@@ -393,7 +393,7 @@ template <typename T, int D, bool VEC>
 hipError_t go_backward(const AttnArgs &a, hipStream_t st)
 {
     static bool done_q[kMaxDevices] = {}, done_kv[kMaxDevices] = {};
-    const size_t row = (size_t)Tile<T, D>::kRowBytes, lut = bias_lut_floats(a);
+    const size_t row = (size_t)Tile<T, row_values(D)>::kRowBytes, lut = bias_lut_floats(a);
     const int64_t q_blocks = (int64_t)a.batch * a.heads * ((a.q_len + kRowTile - 1) / kRowTile) * a.q_parts;
     const int64_t k_blocks = (int64_t)a.batch * a.kv_heads * ((a.k_len + kRowTile - 1) / kRowTile) * a.kv_parts + (a.dtable ? a.heads : 0);
     if (q_blocks > 0) {
@@ -420,10 +420,10 @@ hipError_t go_backward(const AttnArgs &a, hipStream_t st)
 
 }  // namespace
 
-hipError_t launch_join_parts(const JoinJobs &jobs, int dim, egeria_dtype dt, bool vec, hipStream_t st)       // (heads of at most 64)
+hipError_t launch_join_parts(const JoinJobs &jobs, int dim, egeria_dtype dt, bool vec, hipStream_t st)
 {
-    if (dt == EGERIA_F32) return vec ? go_join<float, 64, true>(jobs, dim, st) : go_join<float, 64, false>(jobs, dim, st);
-    return vec ? go_join<uint16_t, 64, true>(jobs, dim, st) : go_join<uint16_t, 64, false>(jobs, dim, st);
+    const AttnArgs a = {.dim = dim};
+    return dt == EGERIA_F32 ? EG_PICK_DIM(go_join, float, vec, a, jobs, dim, st) : EG_PICK_DIM(go_join, uint16_t, vec, a, jobs, dim, st);
 }
 hipError_t launch_attention_backward(const AttnArgs &a, egeria_dtype dt, bool vec, hipStream_t st) { return EG_PICK(go_backward, a, dt, vec, st); }
 

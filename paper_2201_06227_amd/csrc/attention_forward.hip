@@ -14,7 +14,7 @@ namespace {
 template <typename T, int D>
 struct RowState {
     static constexpr int kDepth = D / 16, kBlocks = D / 32;
-    typedef Tile<T, D> tile;
+    typedef Tile<T, row_values(D)> tile;
     typename tile::frag q[kDepth];
     v16f o[kBlocks];
     float m, l;
@@ -94,10 +94,10 @@ __device__ __forceinline__ float largest(const v16f (&s)[N])
 }
 
 template <typename T, int D, bool VEC>
-__global__ __launch_bounds__(256, sizeof(T) * D == 512 ? 1 : 2) void attention_forward_kernel(AttnArgs a)
+__global__ __launch_bounds__(256, sizeof(T) * row_values(D) == 512 ? 1 : 2) void attention_forward_kernel(AttnArgs a)
 {
     extern __shared__ __attribute__((aligned(16))) char smem[];
-    typedef Tile<T, D> tile;
+    typedef Tile<T, row_values(D)> tile;
     constexpr int kTileBytes = kKeyTile * tile::kRowBytes;
     const int tid = threadIdx.x, lane = tid & 63, half = lane >> 5, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const uint32_t tiles = (uint32_t)(a.q_len + kRowTile - 1) / kRowTile;
@@ -206,7 +206,7 @@ __global__ __launch_bounds__(256, sizeof(T) * D == 512 ? 1 : 2) void attention_f
 // where there are few tiles, joined by a second launch.
 
 template <typename T, int D> struct FewLayout {
-    static constexpr int kTileBytes = kFewKeys * Tile<T, D>::kRowBytes;
+    static constexpr int kTileBytes = kFewKeys * Tile<T, row_values(D)>::kRowBytes;
     static constexpr int kBuffers = 4 * 2 * 2 * kTileBytes <= 128 * 1024 ? 2 : 1;
     static constexpr int kWaveBytes = 2 * kBuffers * kTileBytes;
     static constexpr int kRowFloats = D + 4;                                // rows of the joined outputs, on different banks
@@ -265,10 +265,10 @@ __global__ __launch_bounds__(256) void attention_few_kernel(AttnArgs a)
     Feed<T, D, VEC, kFewKeys, 64> kr, vr;
     kr.open(a.k, b, g, nk, a.dim, lane);
     vr.open(a.v, b, g, nk, a.dim, lane);
-    const typename Tile<T, D>::Lane at_lane = Tile<T, D>::lane_at(lds, lane);
+    const typename Tile<T, row_values(D)>::Lane at_lane = Tile<T, row_values(D)>::lane_at(lds, lane);
     if (a.table) __syncthreads();
     const float beta_left = a.table ? my_tab[lut[0]] : 0.0f, beta_right = a.table ? my_tab[lut[a.b.far + lut_hi]] : 0.0f;
-    constexpr int kLoads = 2 * kFewKeys * Tile<T, D>::kUnits / 64;         // requests of one step
+    constexpr int kLoads = 2 * kFewKeys * Tile<T, row_values(D)>::kUnits / 64;         // requests of one step
     int j0 = k0 + kFewKeys * wave;
     auto stage = [&](uint32_t to, int j) {
         asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");                 // the buffer has been read
@@ -375,7 +375,9 @@ __global__ __launch_bounds__(256) void attention_few_kernel(AttnArgs a)
 template <typename T, int D, bool VEC>
 __global__ __launch_bounds__(256) void attention_join_kernel(AttnArgs a, uint32_t row_tiles)
 {
-    const uint32_t rows = (uint32_t)a.group * (uint32_t)a.q_len, per = 256 / (D / 4);
+    constexpr uint32_t per = 256 / (D / 4);
+    const uint32_t rows = (uint32_t)a.group * (uint32_t)a.q_len;
+    if (threadIdx.x >= per * (D / 4)) return;
     const int64_t n = (int64_t)xcd_piece(blockIdx.x, gridDim.x) * per + threadIdx.x / (D / 4);       // row of all tiles
     const int f = threadIdx.x % (D / 4) * 4;
     const int64_t tile = n / kFewRows;
@@ -427,7 +429,7 @@ template <typename T, int D, bool VEC>
 hipError_t go(const AttnArgs &a, hipStream_t st)
 {
     static bool done[kMaxDevices] = {};
-    const size_t lds = 4 * (size_t)kKeyTile * Tile<T, D>::kRowBytes + 4 * bias_lut_floats(a);
+    const size_t lds = 4 * (size_t)kKeyTile * Tile<T, row_values(D)>::kRowBytes + 4 * bias_lut_floats(a);
     const hipError_t e = allow_lds(attention_forward_kernel<T, D, VEC>, lds, done);
     if (e != hipSuccess) return e;
     const int64_t blocks = (int64_t)a.batch * a.heads * ((a.q_len + kRowTile - 1) / kRowTile);

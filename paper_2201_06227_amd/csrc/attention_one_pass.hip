@@ -62,20 +62,20 @@ __device__ __forceinline__ v4f mma16(v4f a, v4f b, v4f c)
 
 // LDS of a workgroup: keys, dS of a step, two pairs of query tiles, then the bias and the sums by distance
 template <typename T, int WAVES> struct OnePass {
-    static constexpr int D = 64, kQueries = 128 / (int)sizeof(T);           // queries of a step: a row of dS^T has 128 bytes
-    typedef Tile<T, D> tile;
+    static constexpr int kQueries = 128 / (int)sizeof(T);           // queries of a step: a row of dS^T has 128 bytes
+    typedef Tile<T, 64> tile;
     typedef Tile<T, kQueries> ds_tile;
     static constexpr int kTileBytes = kQueries * tile::kRowBytes, kKeyBytes = 32 * WAVES * tile::kRowBytes, kDsBytes = 32 * WAVES * 128;
     static constexpr int kStage = kKeyBytes + kDsBytes + 4 * kTileBytes;
 };
 
-template <typename T, bool VEC, int WAVES>
+template <typename T, int D, bool VEC, int WAVES>
 __global__ __launch_bounds__(64 * WAVES, 2) void attention_one_pass_kernel(AttnArgs a)
 {
     extern __shared__ __attribute__((aligned(16))) char smem[];
     typedef OnePass<T, WAVES> L;
     typedef typename L::tile tile;
-    constexpr int D = 64, kQueries = L::kQueries, kTileBytes = L::kTileBytes, kThreads = 64 * WAVES;
+    constexpr int kQueries = L::kQueries, kTileBytes = L::kTileBytes, kThreads = 64 * WAVES;
     constexpr int kLanesPerRow = tile::kUnits, kRowsAtOnce = kThreads / kLanesPerRow, kRounds = kQueries / kRowsAtOnce;
     __shared__ float stat[2][2][kQueries];                                  // base-2 log-sum-exp and delta of a step's queries
     const int tid = threadIdx.x, lane = tid & 63, half = lane >> 5, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -144,9 +144,9 @@ __global__ __launch_bounds__(64 * WAVES, 2) void attention_one_pass_kernel(AttnA
         }
     };
     typename tile::frag k[D / 16], v[D / 16];
-    v16f dk[2], dv[2];
+    v16f dk[D / 32], dv[D / 32];
 #pragma unroll
-    for (int n = 0; n < 2; ++n) dk[n] = dv[n] = v16f(0.0f);
+    for (int n = 0; n < D / 32; ++n) dk[n] = dv[n] = v16f(0.0f);
     if (begin < steps) {
         Feed<T, D, VEC, 32 * WAVES, kThreads> keys;
         keys.open(a.k, b, hk, nk, a.dim, tid);
@@ -270,7 +270,7 @@ __global__ __launch_bounds__(64 * WAVES, 2) void attention_one_pass_kernel(AttnA
                     for (int e = 0; e < 2; ++e) {
                         const typename tile::frag fp = pack<T>(p, e), fs = pack<T>(s, e);
 #pragma unroll
-                        for (int m = 0; m < 2; ++m) {
+                        for (int m = 0; m < D / 32; ++m) {
                             dv[m] = mma(tile::col_frag(at, now + kTileBytes, 32 * n + 16 * e, m), fp, dv[m]);
                             dk[m] = mma(tile::col_frag(at, now, 32 * n + 16 * e, m), fs, dk[m]);
                         }
@@ -285,19 +285,19 @@ __global__ __launch_bounds__(64 * WAVES, 2) void attention_one_pass_kernel(AttnA
         // dQ^T of the step, 16 features of 16 queries at a time, over all keys: a wave's blocks have the same features, so they share
         // the keys' fragments; several chunks of keys are read ahead of their products (one at a time the waits for LDS made this 1.5 us
         // of a step's 5)
-        constexpr int kBlocks = kQueries / 4, kMine = kBlocks / WAVES, kAhead = 4;
-        const int mb = wave & 3;
+        constexpr int kWide = D / 16, kBlocks = kWide * (kQueries / 16), kMine = kBlocks > WAVES ? kBlocks / WAVES : 1, kAhead = 4;
+        const int mb = wave % kWide;
         v4f x[kMine];
 #pragma unroll
         for (int t = 0; t < kMine; ++t) x[t] = v4f(0.0f);
-        for (int n0 = 0; n0 < chunks; n0 += kAhead) {
+        for (int n0 = 0; n0 < chunks && wave < kBlocks; n0 += kAhead) {
             typename Across<T, 8>::frag fk[kAhead], fd[kMine][kAhead];
 #pragma unroll
             for (int n = 0; n < kAhead; ++n) {
                 const int r0 = (n0 + n < chunks ? n0 + n : n0) * Across<T, 8>::kRows;
                 fk[n] = Across<T, tile::kUnits>::get(at_k, r0, mb);
 #pragma unroll
-                for (int t = 0; t < kMine; ++t) fd[t][n] = Across<T, 8>::get(at_ds, r0, (wave + WAVES * t) >> 2);
+                for (int t = 0; t < kMine; ++t) fd[t][n] = Across<T, 8>::get(at_ds, r0, (wave + WAVES * t) / kWide);
             }
 #pragma unroll
             for (int n = 0; n < kAhead; ++n)
@@ -308,8 +308,8 @@ __global__ __launch_bounds__(64 * WAVES, 2) void attention_one_pass_kernel(AttnA
         }
 #pragma unroll
         for (int t = 0; t < kMine; ++t) {
-            const int i = i0 + 16 * ((wave + WAVES * t) >> 2) + (lane & 15);
-            if (i < a.q_len) {
+            const int i = i0 + 16 * ((wave + WAVES * t) / kWide) + (lane & 15);
+            if (wave < kBlocks && i < a.q_len) {
                 T *out = (T *)a.dq.p + ((int64_t)b * a.dq.sb + (int64_t)i * a.dq.st + (int64_t)h * a.dq.sh);
                 const float sc = i < nq ? a.scale : 0.0f;
                 store4<T, VEC>(out, 16 * mb + 4 * (lane >> 4), a.dim, x[t][0] * sc, x[t][1] * sc, x[t][2] * sc, x[t][3] * sc);
@@ -340,7 +340,7 @@ __global__ __launch_bounds__(64 * WAVES, 2) void attention_one_pass_kernel(AttnA
     __syncthreads();                                                        // the keys have been read
     if (j >= nk) {                                                          // (columns of their own, and anything may be in them)
 #pragma unroll
-        for (int n = 0; n < 2; ++n) dk[n] = dv[n] = v16f(0.0f);
+        for (int n = 0; n < D / 32; ++n) dk[n] = dv[n] = v16f(0.0f);
     }
     if (parts == 1) {
         const uint32_t room = lds + 32 * wave * tile::kRowBytes;
@@ -349,7 +349,7 @@ __global__ __launch_bounds__(64 * WAVES, 2) void attention_one_pass_kernel(AttnA
     } else if (j < a.k_len) {
         float *sum = a.part_kv + (((int64_t)part * (a.batch * a.kv_heads - a.whole) + (bh - a.whole)) * a.k_len + j) * (2 * D);
 #pragma unroll
-        for (int n = 0; n < 2; ++n)
+        for (int n = 0; n < D / 32; ++n)
 #pragma unroll
             for (int r = 0; r < 16; r += 4) {
                 const int f = 32 * n + row_of(r, half);
@@ -367,20 +367,20 @@ size_t lds_of(const Buckets *b, bool table_grad)
     return n;
 }
 
-template <typename T, bool VEC, int WAVES>
+template <typename T, int D, bool VEC, int WAVES>
 hipError_t go_one_pass(const AttnArgs &a, hipStream_t st)
 {
     static bool done[kMaxDevices] = {};
     const size_t lds = lds_of<T, WAVES>(a.table ? &a.b : nullptr, a.partials != nullptr);
-    hipError_t e = allow_lds(attention_one_pass_kernel<T, VEC, WAVES>, lds, done);
+    hipError_t e = allow_lds(attention_one_pass_kernel<T, D, VEC, WAVES>, lds, done);
     if (e != hipSuccess) return e;
     const int64_t over = (int64_t)a.batch * a.kv_heads - a.whole;
-    e = launch_k(EGERIA_KERNEL_ATTENTION, attention_one_pass_kernel<T, VEC, WAVES>, dim3((unsigned)(a.whole + over * a.kv_parts)), dim3(64 * WAVES), lds,
+    e = launch_k(EGERIA_KERNEL_ATTENTION, attention_one_pass_kernel<T, D, VEC, WAVES>, dim3((unsigned)(a.whole + over * a.kv_parts)), dim3(64 * WAVES), lds,
                  st, a);
     if (e != hipSuccess) return e;
     JoinJobs jobs;
-    jobs.add({a.dk, a.part_kv, over * a.k_len, a.kv_heads, a.k_len, a.kv_parts, 128, a.whole});
-    jobs.add({a.dv, a.part_kv + 64, over * a.k_len, a.kv_heads, a.k_len, a.kv_parts, 128, a.whole});
+    jobs.add({a.dk, a.part_kv, over * a.k_len, a.kv_heads, a.k_len, a.kv_parts, 2 * D, a.whole});
+    jobs.add({a.dv, a.part_kv + D, over * a.k_len, a.kv_heads, a.k_len, a.kv_parts, 2 * D, a.whole});
     e = launch_join_parts(jobs, a.dim, sizeof(T) == 4 ? EGERIA_F32 : EGERIA_BF16, VEC, st);
     if (e != hipSuccess || !a.dtable) return e;
     return launch_table_reduce(a.partials, a.heads, a.table_parts, a.table_rows, a.dtable, st);
@@ -397,14 +397,22 @@ size_t one_pass_lds(const egeria_attention_desc *d, bool table_grad)
     return d->k_len <= 128 ? lds_of<uint16_t, 4>(p, table_grad) : lds_of<uint16_t, 8>(p, table_grad);
 }
 
+namespace {
+
+template <typename T, int D, bool VEC>
+hipError_t go_keys(const AttnArgs &a, hipStream_t st) { return a.k_len <= 128 ? go_one_pass<T, D, VEC, 4>(a, st) : go_one_pass<T, D, VEC, 8>(a, st); }
+template <typename T>
+hipError_t go_dim(const AttnArgs &a, bool vec, hipStream_t st)
+{
+    if (a.dim <= 32) return vec ? go_keys<T, 32, true>(a, st) : go_keys<T, 32, false>(a, st);
+    return vec ? go_keys<T, 64, true>(a, st) : go_keys<T, 64, false>(a, st);
+}
+
+}  // namespace
+
 hipError_t launch_attention_one_pass(const AttnArgs &a, egeria_dtype dt, bool vec, hipStream_t st)
 {
-    if (dt == EGERIA_F32) {
-        if (a.k_len <= 128) return vec ? go_one_pass<float, true, 4>(a, st) : go_one_pass<float, false, 4>(a, st);
-        return vec ? go_one_pass<float, true, 8>(a, st) : go_one_pass<float, false, 8>(a, st);
-    }
-    if (a.k_len <= 128) return vec ? go_one_pass<uint16_t, true, 4>(a, st) : go_one_pass<uint16_t, false, 4>(a, st);
-    return vec ? go_one_pass<uint16_t, true, 8>(a, st) : go_one_pass<uint16_t, false, 8>(a, st);
+    return dt == EGERIA_F32 ? go_dim<float>(a, vec, st) : go_dim<uint16_t>(a, vec, st);
 }
 
 }  // namespace egeria

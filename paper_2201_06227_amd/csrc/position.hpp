@@ -158,6 +158,7 @@ __device__ __forceinline__ void reduce_table(const float *__restrict__ partials,
     memory[threadIdx.x] = s;
     __syncthreads();
     if (g == 0 && n < buckets) {
+#pragma unroll 8
         for (int k = 1; k < groups; ++k) s += memory[k * width + n];
         dtable[n * heads + h] = (float)s;
     }
