@@ -91,13 +91,14 @@ int64_t few_tiles(const egeria_attention_desc *d)
 }
 
 // The forward kernel for few rows, and how many workgroups share a row tile's keys there (0: the other kernel).  A tile of 128 queries
-// leaves most of its waves without rows up to 32 queries; and where the tiles are few and the keys many, the keys have to be shared
-// to occupy the device.  Splits have at least 256 keys.
+// leaves most of its waves without rows up to 32 queries; and where there are few such tiles, tiles of 32 rows and a share of the
+// keys for each wave occupy more of the device (128-row tiles / this way, us: fp32 2 x 512 x 6 x 64 40 / 20, bf16 1 x 1000 x 4 x 128 26 /
+// 20, 2 x 512 x 6 x 64 causal 14 / 14, 7 x 64 x 8 x 64 6 / 7, 1 x 2048 x 3 x 128 46 / 51).  Splits have at least 256 keys.
 int few_splits(const egeria_attention_desc *d)
 {
     const int64_t blocks = (int64_t)d->batch * d->heads * (((int64_t)d->q_len + kRowTile - 1) / kRowTile);
     const int64_t tiles = few_tiles(d);
-    if (d->q_len > 32 && blocks >= 64) return 0;
+    if (d->q_len > 32 && !(blocks < 48 && d->k_len >= (d->dtype == EGERIA_F32 ? 64 : 512))) return 0;
     if (tiles == 0) return 0;
     // a round of workgroups, if their keys are few; else two, since the sequences' lengths may differ
     const int64_t slots = (int64_t)compute_units() * (d->dtype == EGERIA_BF16 && d->head_dim <= 64 ? 2 : 1);
