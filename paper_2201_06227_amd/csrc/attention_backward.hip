@@ -70,7 +70,9 @@ __global__ __launch_bounds__(256, sizeof(T) * row_values(D) == 512 ? 1 : 2) void
         q[kk] = qr.frag(qw, kk, lane);
         g[kk] = gr.frag(qw, kk, lane);
         delta += dot(g[kk], orow.frag(qw, kk, lane));
+        g[kk] = turned(g[kk], lane);
     }
+    const float sign = sign_of<typename tile::frag>(lane);
     delta += lane_xor<32>(delta);
     if (half == 0 && i < a.q_len && part == 0) a.delta[row] = delta;
     const float lse = i < nq ? a.lse[row] : -INFINITY;
@@ -78,7 +80,7 @@ __global__ __launch_bounds__(256, sizeof(T) * row_values(D) == 512 ? 1 : 2) void
     v16f dq[D / 32];
 #pragma unroll
     for (int n = 0; n < D / 32; ++n) dq[n] = v16f(0.0f);
-    float left = 0.0f, right = 0.0f;                                        // sums of ds beyond the table by distance
+    double left = 0.0, right = 0.0;                                         // sums of ds beyond the table by distance: long ones, of values that cancel
     if (bias.on) __syncthreads();
     bias.fill(a);
 
@@ -120,20 +122,17 @@ __global__ __launch_bounds__(256, sizeof(T) * row_values(D) == 512 ? 1 : 2) void
                 }
             }
 #pragma unroll
-            for (int r = 0; r < 16; ++r) s[r] *= d[r] - delta;
+            for (int r = 0; r < 16; ++r) s[r] *= fmaf(sign, d[r], -delta);
             if (edge) {
-const int live = nk - jn - 4 * half, most = a.causal && -rel < live - 1 ? -rel + 1 : live;
+                const int live = nk - jn - 4 * half, most = a.causal && -rel < live - 1 ? -rel + 1 : live;
 #pragma unroll
                 for (int r = 0; r < 16; ++r)
                     if (row_of(r, 0) >= most) s[r] = 0.0f;
             }
             if (a.partials) {
                 if (one) {
-                    float sum = 0.0f;
-#pragma unroll
-                    for (int r = 0; r < 16; ++r) sum += s[r];
-                    if (bias.left(hi)) left += sum;
-                    else right += sum;
+                    if (bias.left(hi)) left += (double)sum16(s);
+                    else right += (double)sum16(s);
                 } else add_diagonals<1>(s, mine + (jn - qw - shift + bias.far + kPad), lane);
             }
 #pragma unroll
@@ -164,8 +163,8 @@ const int live = nk - jn - 4 * half, most = a.causal && -rel < live - 1 ? -rel +
         left = wave_sum(left);
         right = wave_sum(right);
         if (lane == 0) {                                                   // the wave's own table: in order after its additions
-            mine[0] += left;
-            mine[entries - 1] += right;
+            mine[0] += (float)left;
+            mine[entries - 1] += (float)right;
         }
         bucket_sums(bias.spans, sums, 8, entries, entries, a.table_rows, a.partials + (((int64_t)h * a.batch + b) * a.q_parts * tiles + part * tiles + rt) * a.table_rows);
     }

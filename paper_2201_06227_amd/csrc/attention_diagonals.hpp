@@ -4,6 +4,23 @@
 
 namespace egeria {
 
+// The bf16 products round towards minus infinity on the average, by 1e-9 of operands of size one, which a table's gradient, a long sum
+// of p (dP - delta) that cancels, would gather.  So every other row or column of dP is made with the opposite sign: `turned` is its operand,
+// `sign_of` what the product is taken by.
+template <typename F>
+__device__ __forceinline__ F turned(F f, int index)
+{
+    if constexpr (sizeof(F) == 16) return __builtin_bit_cast(F, __builtin_bit_cast(v4u, f) ^ v4u((index & 1) ? 0x80008000u : 0u));
+    else return f;                                                          // fp32: exact halves are as often up as down
+}
+template <typename F>
+__device__ __forceinline__ float sign_of(int index) { return sizeof(F) == 16 && (index & 1) ? -1.0f : 1.0f; }
+
+__device__ __forceinline__ float sum16(const v16f &s)
+{
+    return (((s[0] + s[1]) + (s[2] + s[3])) + ((s[4] + s[5]) + (s[6] + s[7]))) + (((s[8] + s[9]) + (s[10] + s[11])) + ((s[12] + s[13]) + (s[14] + s[15])));
+}
+
 // Adds a block of dS to sums by distance: into[d] for d = key - query of the block.  SIGN 1: dS^T (keys down, queries across); -1: dS.
 // (In terms of the former:) A value in lane l of a row of 16 lanes and register r has distance u - l, u being the register's key modulo 16, up to multiples of
 // 16 and of the half's 4 that all lanes of the row share.  Moved down by u lanes, values of one distance lie in one lane, those

@@ -93,7 +93,7 @@ __global__ __launch_bounds__(64 * WAVES, 2) void attention_one_pass_kernel(AttnA
     const int entries = bias.count();
     float *sums = bias.end(), *mine = sums + (2 * wave + half) * entries;  // [wave][half]: sums of ds by distance
     const int jw = 32 * wave, j = jw + (lane & 31);
-    const float c = a.scale * kLog2e;
+    const float c = a.scale * kLog2e, sign = sign_of<typename tile::frag>(lane);
 
     Feed<T, D, VEC, kQueries, kThreads> qr, gr;
     qr.open(a.q, b, 0, nq, a.dim, tid);
@@ -158,25 +158,25 @@ __global__ __launch_bounds__(64 * WAVES, 2) void attention_one_pass_kernel(AttnA
 #pragma unroll
         for (int kk = 0; kk < D / 16; ++kk) {
             k[kk] = kr.frag(jw, kk, lane);
-            v[kk] = vr.frag(jw, kk, lane);
+            v[kk] = turned(vr.frag(jw, kk, lane), lane);
         }
         asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
         keep(0);
     }
     const typename tile::Lane at = tile::lane_at(lds_q, lane);
     const uint32_t at_k = Across<T, tile::kUnits>::lane_at(lds, lane), at_ds = Across<T, 8>::lane_at(lds_ds, lane);
-    float left = 0.0f, right = 0.0f;
+    double left = 0.0, right = 0.0;                                         // sums of ds beyond the table by distance: long ones, of values that cancel
     int lut_head = -1;
     auto table_sums = [&](int h, int q) { return a.partials + (((int64_t)h * a.batch + b) * a.kv_parts + q) * a.table_rows; };
     auto finish_head = [&](int h) {                                         // the sums by bucket of a head whose queries are done
         left = wave_sum(left);
         right = wave_sum(right);
         if (lane == 0) {
-            mine[0] += left;
-            mine[entries - 1] += right;
+            mine[0] += (float)left;
+            mine[entries - 1] += (float)right;
         }
         bucket_sums<kThreads>(bias.spans, sums, 2 * WAVES, entries, entries, a.table_rows, table_sums(h, part));
-        left = right = 0.0f;
+        left = right = 0.0;
         __syncthreads();
     };
 
@@ -237,15 +237,12 @@ __global__ __launch_bounds__(64 * WAVES, 2) void attention_one_pass_kernel(AttnA
                         const float4 delta = *(const float4 *)&stat[kBuffer][1][32 * n + row_of(r, half)];
                         const float ds[4] = {delta.x, delta.y, delta.z, delta.w};
 #pragma unroll
-                        for (int e = 0; e < 4; ++e) s[r + e] = p[r + e] * (d[r + e] - ds[e]);
+                        for (int e = 0; e < 4; ++e) s[r + e] = p[r + e] * fmaf(sign, d[r + e], -ds[e]);
                     }
                     if (a.partials) {
                         if (one) {
-                            float sum = 0.0f;
-#pragma unroll
-                            for (int r = 0; r < 16; ++r) sum += s[r];
-                            if (bias.left(hi)) left += sum;
-                            else right += sum;
+                            if (bias.left(hi)) left += (double)sum16(s);
+                            else right += (double)sum16(s);
                         } else add_diagonals<-1>(s, mine + (jw - in - shift + bias.far + kPad), lane);
                     }
                 }
