@@ -109,14 +109,22 @@ int few_splits(const egeria_attention_desc *d)
     return n < 1 ? 1 : (int)n;
 }
 
-// Parts that the steps of a backward kernel's workgroups are dealt in where there are few of them, each a sum in fp32 that a last
-// launch adds up: as many as `slots` workgroups make, of two steps at least, at most 16.
-int parts_of(int64_t blocks, int64_t steps, int64_t slots)
+// Parts that the steps of a backward kernel's workgroups are dealt in, each a sum in fp32 that a last launch adds up: the number, at
+// most 16 and of two steps at least, that ends first when `slots` workgroups run at a time.  A workgroup costs two steps more than it
+// has, the last launch two.  Causal: half the steps in all, but the longest workgroup has all of its own.
+int parts_of(int64_t blocks, int64_t steps, int64_t slots, bool causal)
 {
-    if (blocks == 0) return 1;
-    int64_t n = slots / blocks;
-    n = n > steps / 2 ? steps / 2 : n;
-    return n < 1 ? 1 : (n > 16 ? 16 : (int)n);
+    int best = 1;
+    double least = 0.0;
+    for (int n = 1; n <= 16 && (n == 1 || 2 * n <= steps); ++n) {
+        const double rounds = (double)((blocks * n + slots - 1) / slots), each = (double)((steps + n - 1) / n), all = 0.5 * (double)blocks * (double)steps / (double)slots;
+        const double cost = (causal ? (all > each ? all : each) + 2.0 * rounds : rounds * (each + 2.0)) + (n > 1 ? 2.0 : 0.0);
+        if (n == 1 || cost < least) {
+            best = n;
+            least = cost;
+        }
+    }
+    return best;
 }
 
 // The backward kernel that makes everything in one pass: where its keys and LDS fit and a workgroup for each key head of the batch
@@ -139,11 +147,11 @@ Plan make_plan(const egeria_attention_desc *d, bool backward)
     if (backward && one_pass(d)) {
         p.one = true;
         // rounds of as many key heads as run at a time; what the last round would have fewer of is done in parts, so that it is short
-        const int64_t units = (int64_t)d->batch * d->kv_heads, slots = (int64_t)compute_units() * (d->k_len <= 128 ? 2 : 1);
+        const int64_t units = (int64_t)d->batch * d->kv_heads, slots = (int64_t)compute_units() * (d->k_len <= 128 ? 2 : 1), over = units % slots;
         const int64_t steps = ((int64_t)d->q_len + one_pass_queries(d->dtype) - 1) / one_pass_queries(d->dtype) * (d->heads / d->kv_heads);
-        const int64_t over = units % slots;
-        int64_t parts = over && units > slots ? slots / over : 1;
-        parts = parts > steps ? steps : parts;
+        int64_t parts = over ? slots / over : 1;
+        const int64_t most = units > slots ? steps : steps / 2;            // (a sum in parts costs a launch: for half a round's steps at least)
+        parts = parts > most ? most : parts;
         p.kv_parts = (int)(parts < 1 ? 1 : (parts > 16 ? 16 : parts));
         p.whole = (int)(p.kv_parts > 1 ? units - over : units);
         p.off_part = take((size_t)d->batch * d->heads * p.kv_parts * position_rows(d->bias) * 4);
@@ -152,10 +160,14 @@ Plan make_plan(const egeria_attention_desc *d, bool backward)
     }
     if (backward) {
         p.off_delta = take((size_t)d->batch * d->heads * d->q_len * 4);
-        const int64_t key_tiles = ((int64_t)d->k_len + kRowTile - 1) / kRowTile, wide = padded_dim(d->head_dim);
-        p.q_parts = parts_of((int64_t)d->batch * d->heads * row_tiles(d), key_tiles * kRowTile / kKeyTile, 2 * (int64_t)compute_units());
-        p.kv_parts = parts_of((int64_t)d->batch * d->kv_heads * key_tiles, row_tiles(d) * kRowTile / kKeyTile * (d->heads / d->kv_heads),
-                              (d->causal ? 4 : 2) * (int64_t)compute_units());         // (causal: pieces of unlike length, two rounds)
+        const int64_t key_tiles = ((int64_t)d->k_len + kRowTile - 1) / kRowTile, wide = padded_dim(d->head_dim), cu = compute_units();
+        // workgroups of the two kernels that a compute unit holds, by their LDS and registers
+        const bool f32 = d->dtype == EGERIA_F32, long_rows = d->head_dim > 64;
+        const int64_t q_slots = cu * (f32 ? (long_rows ? 1 : 2) : (long_rows ? 2 : 3)), kv_slots = cu * (f32 && long_rows ? 1 : 2);
+        const int64_t q_steps = ((int64_t)d->k_len + kKeyTile - 1) / kKeyTile, kv_step = long_rows ? kKeyTile / 2 : kKeyTile;
+        p.q_parts = parts_of((int64_t)d->batch * d->heads * row_tiles(d), q_steps, q_slots, d->causal != 0);
+        p.kv_parts = parts_of((int64_t)d->batch * d->kv_heads * key_tiles, ((int64_t)d->q_len + kv_step - 1) / kv_step * (d->heads / d->kv_heads), kv_slots,
+                              d->causal != 0);
         p.off_part = take((size_t)d->batch * d->heads * row_tiles(d) * p.q_parts * position_rows(d->bias) * 4);
         if (p.q_parts > 1) p.off_q = take((size_t)p.q_parts * d->batch * d->heads * d->q_len * wide * 4);
         if (p.kv_parts > 1) p.off_kv = take((size_t)p.kv_parts * d->batch * d->kv_heads * d->k_len * wide * 8);
