@@ -536,7 +536,8 @@ typedef struct {
  * dtype whose features are contiguous; strides in elements, not negative.  The
  * data pointer needs the alignment of its type only (16 bytes, with strides in
  * whole units of 16 bytes and head_dim * size a multiple of 16, is faster).
- * Strides of inputs may be 0; elements of outputs must not overlap. */
+ * Strides of inputs may be 0; elements of outputs must not overlap each other
+ * or an input. */
 typedef struct {
     void *data;
     int64_t batch_stride, token_stride, head_stride;
@@ -560,8 +561,9 @@ size_t egeria_attention_workspace_bytes(const egeria_attention_desc *desc, int32
 /* out: [batch, q_len, heads, head_dim].  lse: fp32 [batch, heads, q_len], L of every row.
  * Errors: EGERIA_ERR_INVALID_ARG for a bad descriptor or table, a null or
  * misaligned pointer, a negative stride, an output whose elements overlap;
- * EGERIA_ERR_UNSUPPORTED for head_dim > 128 or sizes beyond 2^31 workgroups or
- * 2^62 bytes; EGERIA_ERR_WORKSPACE_TOO_SMALL. */
+ * EGERIA_ERR_UNSUPPORTED for head_dim > 128, heads > 65535, lengths beyond 2^29,
+ * tensors beyond 2^62 bytes, or a launch beyond 2^32 threads (2^24 tiles of 128
+ * rows); EGERIA_ERR_WORKSPACE_TOO_SMALL. */
 egeria_status egeria_attention(const egeria_attention_desc *desc, const egeria_heads *q, const egeria_heads *k,
                                const egeria_heads *v, const egeria_heads *out, float *lse, void *ws, size_t ws_bytes,
                                void *stream);
@@ -576,7 +578,9 @@ egeria_status egeria_attention_backward(const egeria_attention_desc *desc, const
 /* The bias as a tensor, for attention that is not computed here:
  * bias[h, i, j] = table[bucket(j - i - offset), h], rounded once to dt;
  * bias [heads, q_len, k_len] out, offset the position of query 0 among the keys.
- * |offset| <= 2^29, q_len and k_len <= 2^28, heads <= 65535. */
+ * |offset| <= 2^29, q_len and k_len <= 2^28, heads <= 65535;
+ * EGERIA_ERR_UNSUPPORTED beyond a launch of 2^32 threads (here and in the
+ * gradient; a thread has 8 rows of 16 bytes). */
 egeria_status egeria_position_bias(const egeria_position_table *t, int32_t heads, int32_t q_len, int32_t k_len, int32_t offset,
                                    void *bias, egeria_dtype dt, void *stream);
 

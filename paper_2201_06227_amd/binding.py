@@ -9,6 +9,7 @@ from __future__ import annotations
 import ctypes
 import functools
 import math
+import operator
 import os
 import struct
 from dataclasses import dataclass
@@ -702,6 +703,14 @@ class ActivationCache:
 
 # ---- attention of the training model -----------------------------------------------------------
 
+def _int32(n: int) -> int:
+    """An argument that a C int holds (ctypes would drop the rest)."""
+    n = operator.index(n)
+    if not -(1 << 31) <= n < 1 << 31:
+        raise ValueError(f"{n} is out of range")
+    return n
+
+
 class PositionBias(NamedTuple):
     """A learned bias by relative position: table fp32 [buckets, heads] (egeria_position_table)."""
     table: torch.Tensor
@@ -712,7 +721,7 @@ class PositionBias(NamedTuple):
         t = _dev(self.table)
         if t.dtype != torch.float32 or t.dim() != 2:
             raise ValueError("a position table is fp32 [buckets, heads]")
-        return PositionTable(t.data_ptr(), t.shape[0], int(self.max_distance), 1 if self.bidirectional else 0)
+        return PositionTable(t.data_ptr(), t.shape[0], _int32(self.max_distance), 1 if self.bidirectional else 0)
 
 
 # The calls below are short beside the host's work for them, which is all of a small call's time: descriptors are packed as bytes
@@ -800,7 +809,8 @@ def attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, causal: bool = 
               bias: Optional[PositionBias] = None, out: Optional[torch.Tensor] = None, lse: Optional[torch.Tensor] = None,
               ws: Optional[torch.Tensor] = None):
     """egeria_attention: q [batch, q_len, heads, dim], k and v [batch, k_len, kv_heads, dim] (any strides with contiguous
-    features) -> out like q, and lse fp32 [batch, heads, q_len].  scale: 1 / sqrt(dim) if not given."""
+    features) -> out like q, and lse fp32 [batch, heads, q_len].  scale: 1 / sqrt(dim) if not given.  No autograd: the gradient is
+    attention_backward's."""
     dev = _same_device(q, k, v, q_lens, k_lens, out, lse, ws, None if bias is None else bias.table)
     desc, sizes, _tab = _attention_desc(q, k, v, causal, scale, q_lens, k_lens, bias)
     batch, q_len, heads, _ = q.shape
@@ -863,7 +873,7 @@ def position_bias(bias: PositionBias, q_len: int, k_len: int, offset: int = 0, d
         out = torch.empty((heads, q_len, k_len), dtype=dtype, device=bias.table.device)
     elif _dev(out).shape != (heads, q_len, k_len) or out.dtype != dtype:
         raise ValueError("out must be [heads, q_len, k_len] of dtype")
-    rc = lib().egeria_position_bias(tab, heads, q_len, k_len, int(offset), _ptr(out), _dt(out), _stream())
+    rc = lib().egeria_position_bias(tab, heads, _int32(q_len), _int32(k_len), _int32(offset), _ptr(out), _dt(out), _stream())
     _check(rc, "egeria_position_bias")
     return out
 
@@ -879,7 +889,7 @@ def position_bias_backward(dbias: torch.Tensor, bias: PositionBias, offset: int 
     dtable = torch.empty_like(bias.table)
     if ws is None:
         ws = workspace(int(lib().egeria_position_bias_workspace_bytes(tab, batch, heads, q_len, k_len, _dt(dbias))), dbias.device)
-    rc = lib().egeria_position_bias_backward(tab, _ptr(_dev(dbias)), _dt(dbias), batch, heads, q_len, k_len, int(offset),
+    rc = lib().egeria_position_bias_backward(tab, _ptr(_dev(dbias)), _dt(dbias), batch, heads, q_len, k_len, _int32(offset),
                                              _ptr(dtable), _ptr(ws), ws.numel(), _stream())
     _check(rc, "egeria_position_bias_backward")
     return dtable

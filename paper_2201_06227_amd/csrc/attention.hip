@@ -111,14 +111,18 @@ int few_splits(const egeria_attention_desc *d)
 
 // Parts that the steps of a backward kernel's workgroups are dealt in, each a sum in fp32 that a last launch adds up: the number, at
 // most 16 and of two steps at least, that ends first when `slots` workgroups run at a time.  A workgroup costs two steps more than it
-// has, the last launch two.  Causal: half the steps in all, but the longest workgroup has all of its own.
-int parts_of(int64_t blocks, int64_t steps, int64_t slots, bool causal)
+// has and, to write and join its part, `more`; the last launch half of that.  Causal: half the steps in all, but the longest workgroup
+// has all of its own.  (As many parts as one round of two workgroups for each compute unit holds / this count, us, backward: bf16
+// causal 1 x 4096 x 9 x 64 203 / 156 and 16384 x 2 (1) x 128 579 / 537, fp32 the former 1196 / 831, 2 x 1049 x 710 keys x 16 (8) x 128 544 /
+// 497; but bf16 8 x 512 x 8 x 75 94 / 102.  Without `more`, bf16 causal 6 x 1024 x 12 x 64 takes 109 instead of 86.)
+int parts_of(int64_t blocks, int64_t steps, int64_t slots, double more, bool causal)
 {
     int best = 1;
     double least = 0.0;
     for (int n = 1; n <= 16 && (n == 1 || 2 * n <= steps); ++n) {
         const double rounds = (double)((blocks * n + slots - 1) / slots), each = (double)((steps + n - 1) / n), all = 0.5 * (double)blocks * (double)steps / (double)slots;
-        const double cost = (causal ? (all > each ? all : each) + 2.0 * rounds : rounds * (each + 2.0)) + (n > 1 ? 2.0 : 0.0);
+        const double one = 2.0 + (n > 1 ? more : 0.0);
+        const double cost = (causal ? (all > each ? all : each) + one * rounds : rounds * (each + one)) + (n > 1 ? 0.5 * more : 0.0);
         if (n == 1 || cost < least) {
             best = n;
             least = cost;
@@ -138,6 +142,7 @@ struct Plan {
     bool one = false;
     size_t off_delta = 0, off_part = 0, off_o = 0, off_ml = 0, off_q = 0, off_kv = 0, total = 0;
     int splits = 0, q_parts = 1, kv_parts = 1, whole = 0;
+    int64_t blocks = 0;                     // workgroups of the largest backward launch
 };
 Plan make_plan(const egeria_attention_desc *d, bool backward)
 {
@@ -154,6 +159,7 @@ Plan make_plan(const egeria_attention_desc *d, bool backward)
         parts = parts > most ? most : parts;
         p.kv_parts = (int)(parts < 1 ? 1 : (parts > 16 ? 16 : parts));
         p.whole = (int)(p.kv_parts > 1 ? units - over : units);
+        p.blocks = p.whole + (units - p.whole) * p.kv_parts;
         p.off_part = take((size_t)d->batch * d->heads * p.kv_parts * position_rows(d->bias) * 4);
         if (p.kv_parts > 1) p.off_kv = take((size_t)p.kv_parts * over * d->k_len * padded_dim(d->head_dim) * 8);
         return p;
@@ -165,10 +171,13 @@ Plan make_plan(const egeria_attention_desc *d, bool backward)
         const bool f32 = d->dtype == EGERIA_F32, long_rows = d->head_dim > 64;
         const int64_t q_slots = cu * (f32 ? (long_rows ? 1 : 2) : (long_rows ? 2 : 3)), kv_slots = cu * (f32 && long_rows ? 1 : 2);
         const int64_t q_steps = ((int64_t)d->k_len + kKeyTile - 1) / kKeyTile, kv_step = long_rows ? kKeyTile / 2 : kKeyTile;
-        p.q_parts = parts_of((int64_t)d->batch * d->heads * row_tiles(d), q_steps, q_slots, d->causal != 0);
+        const double more = f32 ? 0.9 : 3.5;                                // a part's bytes, written and read again, in steps
+        p.q_parts = parts_of((int64_t)d->batch * d->heads * row_tiles(d), q_steps, q_slots, more, d->causal != 0);
         p.kv_parts = parts_of((int64_t)d->batch * d->kv_heads * key_tiles, ((int64_t)d->q_len + kv_step - 1) / kv_step * (d->heads / d->kv_heads), kv_slots,
-                              d->causal != 0);
-        p.off_part = take((size_t)d->batch * d->heads * row_tiles(d) * p.q_parts * position_rows(d->bias) * 4);
+                              more, d->causal != 0);
+        const int64_t q_blocks = (int64_t)d->batch * d->heads * row_tiles(d) * p.q_parts, kv_blocks = (int64_t)d->batch * d->kv_heads * key_tiles * p.kv_parts + d->heads;
+        p.blocks = q_blocks > kv_blocks ? q_blocks : kv_blocks;
+        p.off_part = take((size_t)q_blocks * position_rows(d->bias) * 4);
         if (p.q_parts > 1) p.off_q = take((size_t)p.q_parts * d->batch * d->heads * d->q_len * wide * 4);
         if (p.kv_parts > 1) p.off_kv = take((size_t)p.kv_parts * d->batch * d->kv_heads * d->k_len * wide * 8);
         return p;
@@ -219,7 +228,8 @@ egeria_status egeria_attention(const egeria_attention_desc *desc, const egeria_h
     const Plan p = make_plan(desc, false);
     if (ws_bytes < p.total) return EGERIA_ERR_WORKSPACE_TOO_SMALL;
     if (rows == 0) return EGERIA_OK;
-    if ((p.splits ? few_tiles(desc) : rows / kRowTile + (int64_t)desc->batch * desc->heads) > (1 << 28)) return EGERIA_ERR_UNSUPPORTED;
+    // (the launch that joins splits has fewer threads: 8 for a row of its tiles at most 32, and there are splits where tiles are few)
+    if ((p.splits ? few_tiles(desc) * p.splits : row_tiles(desc) * desc->batch * desc->heads) * 256 > kMostThreads) return EGERIA_ERR_UNSUPPORTED;
     AttnArgs a = make_args(desc);
     a.q = view_of(q), a.k = view_of(k), a.v = view_of(v), a.o = view_of(out);
     a.lse = lse;
@@ -242,12 +252,12 @@ egeria_status egeria_attention_backward(const egeria_attention_desc *desc, const
     for (const egeria_heads *t : {k, v}) EG_TRY(check_view(t, desc, desc->k_len, desc->kv_heads, false));
     EG_TRY(check_view(dq, desc, desc->q_len, desc->heads, true));
     for (const egeria_heads *t : {dk, dv}) EG_TRY(check_view(t, desc, desc->k_len, desc->kv_heads, true));
-    const int64_t rows = (int64_t)desc->batch * desc->heads * desc->q_len, keys = (int64_t)desc->batch * desc->kv_heads * desc->k_len;
+    const int64_t rows = (int64_t)desc->batch * desc->heads * desc->q_len;
     if ((rows > 0 && !lse) || ((uintptr_t)lse & 15u) || !ws || ((uintptr_t)ws & 15u)) return EGERIA_ERR_INVALID_ARG;
     if ((dtable && !desc->bias) || ((uintptr_t)dtable & 15u)) return EGERIA_ERR_INVALID_ARG;
     const Plan p = make_plan(desc, true);
     if (ws_bytes < p.total) return EGERIA_ERR_WORKSPACE_TOO_SMALL;
-    if ((rows > keys ? rows : keys) / kRowTile + (int64_t)desc->batch * desc->heads > (1 << 28)) return EGERIA_ERR_UNSUPPORTED;
+    if (p.blocks * (p.one ? 512 : 256) > kMostThreads) return EGERIA_ERR_UNSUPPORTED;
     AttnArgs a = make_args(desc);
     a.d_o = view_of(dout), a.q = view_of(q), a.k = view_of(k), a.v = view_of(v), a.o = view_of(out);
     a.dq = view_of(dq), a.dk = view_of(dk), a.dv = view_of(dv);

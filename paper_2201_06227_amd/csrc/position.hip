@@ -170,6 +170,7 @@ __global__ __launch_bounds__(256) void position_bias_backward_kernel(Buckets b, 
                 if (rel <= -b.far) left += d[e];
                 else if (rel >= hi) right += d[e];
                 else mine[rel + b.far] += d[e];
+                asm volatile("" ::: "memory");                  // the next entry is another lane's: no read of it before this write
             }
             wave_lds_turn();                                       // the next patch's lanes add where others of this one have
         }
@@ -245,7 +246,7 @@ egeria_status egeria_position_bias(const egeria_position_table *t, int32_t heads
     const Buckets b = make_buckets(t);
     const Deal p = make_deal(1, heads, q_len, k_len, dt == EGERIA_F32 ? 4 : 8);
     const int64_t blocks = (int64_t)p.row_blocks * p.col_blocks * heads;
-    if (blocks > 0x7fffffffLL) return EGERIA_ERR_UNSUPPORTED;
+    if (blocks * 256 > kMostThreads) return EGERIA_ERR_UNSUPPORTED;
     const int entries = distance_entries(b);
     const size_t lds = 4 * (size_t)(entries + entries / 64 + 2) + t->buckets * (sizeof(Span) + 4);
     auto go = [&](auto kernel, auto *out) {
@@ -279,7 +280,7 @@ egeria_status egeria_position_bias_backward(const egeria_position_table *t, cons
     const Buckets b = make_buckets(t);
     const Deal p = make_deal(batch, heads, q_len, k_len, dt == EGERIA_F32 ? 4 : 8);
     const int64_t blocks = parts_of(p) * heads;
-    if (blocks > 0x7fffffffLL) return EGERIA_ERR_UNSUPPORTED;
+    if (blocks * 256 > kMostThreads) return EGERIA_ERR_UNSUPPORTED;
     const size_t lds = 32 * (size_t)distance_entries(b) + t->buckets * sizeof(Span);
     auto go = [&](auto kernel, auto *src) {
         return launch_k(EGERIA_KERNEL_NONE, kernel, dim3((unsigned)blocks), dim3(256), lds, st, b, src, (int64_t)batch, (int)heads, (int)q_len,

@@ -13,6 +13,7 @@ namespace egeria {
 
 constexpr int kMaxBuckets = 128;            // rows of a position table
 constexpr int kMaxDistance = 1024;          // largest max_distance: the tables by distance have to fit LDS
+constexpr int64_t kMostThreads = 0xffffffffLL;          // of a launch
 
 struct Buckets {
     int32_t n;                              // buckets of one side

@@ -225,6 +225,32 @@ def test_binding_refuses_other_tensors(eg):
         eg._attention_desc(q.half(), k.half(), k.half(), False, None, None, None, None)
 
 
+def test_launches_beyond_the_grid(eg):
+    """A launch has fewer than 2^32 threads of 256 to a workgroup: more tiles are refused on the host."""
+    L, fake, big = eg.lib(), ctypes.c_void_p(0x1000), 1 << 62
+    many = desc(eg, batch=1 << 24, heads=1, kv_heads=1, q_len=33, k_len=600, head_dim=1)
+    t = lambda n: eg.Heads(0x1000, n, 1, 1)  # noqa: E731
+    assert L.egeria_attention(many, t(33), t(600), t(600), t(33), fake, fake, big, None) == eg.ERR_UNSUPPORTED
+    one = desc(eg, batch=1 << 24, heads=1, kv_heads=1, q_len=1, k_len=1, head_dim=1)
+    assert L.egeria_attention(one, t(1), t(1), t(1), t(1), fake, fake, big, None) == eg.ERR_UNSUPPORTED
+    for d, nq, nk in ((many, 33, 600), (one, 1, 1)):
+        assert L.egeria_attention_backward(d, t(nq), t(nq), t(nk), t(nk), t(nq), fake, t(nq), t(nk), t(nk), None, fake, big, None) == eg.ERR_UNSUPPORTED
+    tab = eg.PositionTable(0x1000, 32, 128, 1)
+    assert L.egeria_position_bias(tab, 64, 1 << 28, 1, 0, fake, eg.BF16, None) == eg.ERR_UNSUPPORTED
+    assert L.egeria_position_bias_backward(tab, fake, eg.BF16, 1, 64, 1 << 28, 1, 0, fake, fake, big, None) == eg.ERR_UNSUPPORTED
+
+
+def test_integers_beyond_c(eg):
+    """A distance or offset that a C int does not hold is refused, not cut to its low bits."""
+    with pytest.raises(ValueError):
+        eg._int32(1 << 32)
+    with pytest.raises(ValueError):
+        eg._int32(-(1 << 31) - 1)
+    with pytest.raises(TypeError):
+        eg._int32(1.5)
+    assert eg._int32(np.int64(7)) == 7 and eg._int32(-(1 << 31)) == -(1 << 31)
+
+
 # ---- GPU -----------------------------------------------------------------------------------------------------------
 
 SHAPES = [  # batch, q_len, k_len, heads, kv_heads, dim
@@ -284,6 +310,14 @@ def test_attention_many_short_sequences(eg, dtype, shape, causal, bias, lens):
         ql[:4], kl[:4] = [nq, 0, nq, nq], [nk, nk, 0, 1]
     tab = None if bias is None else (table(bias[0], h), bias[1], bias[2])
     run_and_check(eg, dtype, *make(dtype, *shape, seed=b), causal=causal, bias=tab, q_lens=None if ql is None else ql.tolist(), k_lens=None if kl is None else kl.tolist())
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("nq,nk", [(0, 9), (9, 0), (0, 0)])
+def test_attention_many_empty_sequences(eg, dtype, nq, nk):
+    q, k, v, dout = make(dtype, 130, nq, nk, 4, 2, 16, seed=1)
+    run_and_check(eg, dtype, q, k, v, dout, bias=(table(8, 4), 20, True))
 
 
 @pytest.mark.gpu
