@@ -36,7 +36,7 @@ template <> __device__ __forceinline__ uint16_t narrow<uint16_t>(float v)
 // Where a thread's patches lie: 2^lg units of 16 bytes side by side (32 to 256 of them, so that half a wave has one row of patches),
 // 256 / 2^lg patches below each other: `rows` rows to a workgroup, and `cols` times these columns one after the other, so that what
 // a workgroup writes or reads lies close together (long rows in pieces of 4 KiB, 64 of them below each other, were written at
-// 4.9 TB/s; 8 whole rows of 8 KiB at WRITE_RATE).
+// 4.9 TB/s; 8 whole rows of 8 KiB at 5.6).
 struct Deal {
     int lg, rows, cols;
     uint32_t row_blocks, col_blocks, shares;
@@ -92,7 +92,7 @@ __global__ __launch_bounds__(256) void position_bias_kernel(Buckets b, const flo
 // half a wave add to different entries at each step and a wave's additions are in order: the result does not depend on timing.
 // WHOLE: rows are whole units of 16 bytes.  Else a row's 16 bytes come from the two whole units that hold them: loads at other
 // addresses cost 24 % where those are multiples of 4, and at odd multiples of 2 run at a fifth of the rate (13 x 22 x 1142 x 391 in bf16
-// 199 us, now ANY_US).
+// 199 us, now 51).
 template <typename T, bool WHOLE>
 __global__ __launch_bounds__(256) void position_bias_backward_kernel(Buckets b, const T *__restrict__ dbias, int64_t batch, int heads,
                                                                      int q_len, int k_len, int offset, Deal deal, int rows_of_table,

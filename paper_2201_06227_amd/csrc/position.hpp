@@ -88,7 +88,7 @@ __device__ __forceinline__ int entries_of_bucket(const Buckets &b, int row, int 
 
 // The entries of every bucket in a table by distance with `pad` more entries on each side, which belong to the ends' buckets, into LDS:
 // by the first `rows` of the workgroup's threads, all borders in one round trip.  (Looked up where they were needed, one bucket
-// after the other, they took most of a short call's time: dq of 64 x 256 x 12 x 64 57 us, now DQ_SPANS.)
+// after the other, they took most of a short call's time: dq of 64 x 256 x 12 x 64 57 us, now 53.)
 struct Span {
     int at, count;
 };
