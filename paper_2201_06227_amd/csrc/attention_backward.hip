@@ -185,7 +185,7 @@ __global__ __launch_bounds__(256, sizeof(T) * row_values(D) == 512 ? 1 : 2) void
     typedef Tile<T, row_values(D)> tile;
     constexpr int kQueries = dkv_queries<D>(), kTileBytes = kQueries * tile::kRowBytes;
     constexpr bool kValuesInLds = D > 64;
-    __shared__ float stat[2][2][kQueries];                                  // base-2 log-sum-exp and delta of a step's queries
+    __shared__ float stat[2][2][kQueries];                                  // base-2 log-sum-exp and -delta of a step's queries
     const int tid = threadIdx.x, lane = tid & 63, half = lane >> 5, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     // the table's gradient, whose partial sums the dq kernel has left: the first workgroups
     const uint32_t extra = a.dtable ? (uint32_t)a.heads : 0u;
@@ -248,7 +248,7 @@ __global__ __launch_bounds__(256, sizeof(T) * row_values(D) == 512 ? 1 : 2) void
     auto keep = [&](int buffer) {
         if (tid < kQueries) {
             stat[buffer][0][tid] = next_base == -INFINITY ? INFINITY : next_base * kLog2e;
-            stat[buffer][1][tid] = next_delta;
+            stat[buffer][1][tid] = -next_delta;
         }
     };
     if (begin < steps) {
@@ -285,7 +285,14 @@ __global__ __launch_bounds__(256, sizeof(T) * row_values(D) == 512 ? 1 : 2) void
         for (int n = 0; n < kQueries / 32; ++n) {
             const int in = i0 + 32 * n;
             if (in >= nq || jw >= nk || (a.causal && jw > in + 31 + shift)) continue;
-            v16f s = v16f(0.0f), d = v16f(0.0f);
+            // dP - delta: the sum of the products starts at -delta (and no bias, no addition of it: causal 2 x 4096 x 16 (4) x 128 557 us,
+            // now 539)
+            v16f s = v16f(0.0f), d;
+#pragma unroll
+            for (int r = 0; r < 16; r += 4) {
+                const float4 delta = *(const float4 *)&stat[kBuffer][1][32 * n + row_of(r, half)];
+                d[r] = delta.x, d[r + 1] = delta.y, d[r + 2] = delta.z, d[r + 3] = delta.w;
+            }
 #pragma unroll
             for (int kk = 0; kk < D / 16; ++kk) {
                 s = mma(tile::row_frag(at, now, 32 * n, kk), k[kk], s);
@@ -302,6 +309,11 @@ __global__ __launch_bounds__(256, sizeof(T) * row_values(D) == 512 ? 1 : 2) void
             for (int r = 0; r < 16; r += 4) {
                 const float4 base = *(const float4 *)&stat[kBuffer][0][32 * n + row_of(r, half)];
                 const float bs[4] = {base.x, base.y, base.z, base.w};
+                if (!bias.on) {
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) p[r + e] = __builtin_amdgcn_exp2f(fmaf(s[r + e], c, -bs[e]));
+                    continue;
+                }
                 v4f_any t;
                 if (one) t = v4f_any(beta);
                 else t = bias.four(rel - row_of(r, 0) - 3);                // of the keys' distances from four queries, the last first
@@ -314,12 +326,7 @@ __global__ __launch_bounds__(256, sizeof(T) * row_values(D) == 512 ? 1 : 2) void
                     if (rel - row_of(r, 0) > 0) p[r] = 0.0f;
             }
 #pragma unroll
-            for (int r = 0; r < 16; r += 4) {
-                const float4 delta = *(const float4 *)&stat[kBuffer][1][32 * n + row_of(r, half)];
-                const float ds[4] = {delta.x, delta.y, delta.z, delta.w};
-#pragma unroll
-                for (int e = 0; e < 4; ++e) s[r + e] = p[r + e] * (d[r + e] - ds[e]);
-            }
+            for (int r = 0; r < 16; ++r) s[r] = p[r] * d[r];
 #pragma unroll
             for (int e = 0; e < 2; ++e) {
                 const typename tile::frag fp = pack<T>(p, e), fs = pack<T>(s, e);
