@@ -16,6 +16,11 @@ __device__ __forceinline__ F turned(F f, int index)
 template <typename F>
 __device__ __forceinline__ float sign_of(int index) { return sizeof(F) == 16 && (index & 1) ? -1.0f : 1.0f; }
 
+// Base-2 log-sum-exp of a row less a whole number, which the caller gives back as a power of two: exponents s c - L are rounded to the
+// precision of their own size, and that is log2 of the keys where scores are of size one.  (The product is exact inside the fma; the rest
+// is that of log2 e.)
+__device__ __forceinline__ float lowered(float lse, float whole) { return fmaf(lse, 1.92596303e-8f, fmaf(lse, kLog2e, -whole)); }
+
 __device__ __forceinline__ float sum16(const v16f &s)
 {
     return (((s[0] + s[1]) + (s[2] + s[3])) + ((s[4] + s[5]) + (s[6] + s[7]))) + (((s[8] + s[9]) + (s[10] + s[11])) + ((s[12] + s[13]) + (s[14] + s[15])));

@@ -94,6 +94,9 @@ __global__ __launch_bounds__(64 * WAVES, 2) void attention_one_pass_kernel(AttnA
     float *sums = bias.end(), *mine = sums + (2 * wave + half) * entries;  // [wave][half]: sums of ds by distance
     const int jw = 32 * wave, j = jw + (lane & 31);
     const float c = a.scale * kLog2e, sign = sign_of<typename tile::frag>(lane);
+    // p and dS are 2^whole times what they should be, and so are all sums of them
+    const int whole = nk > 1 ? 31 - __builtin_clz(nk) : 0;
+    const float by_p = __uint_as_float((uint32_t)(127 - whole) << 23);
 
     Feed<T, D, VEC, kQueries, kThreads> qr, gr;
     qr.open(a.q, b, 0, nq, a.dim, tid);
@@ -138,7 +141,7 @@ __global__ __launch_bounds__(64 * WAVES, 2) void attention_one_pass_kernel(AttnA
             s += lane_xor<1>(s);
             if (tid % kLanesPerRow == 0) {
                 const int row = r * kRowsAtOnce + tid / kLanesPerRow;
-                stat[buffer][0][row] = next_lse[r] == -INFINITY ? INFINITY : next_lse[r] * kLog2e;
+                stat[buffer][0][row] = next_lse[r] == -INFINITY ? INFINITY : lowered(next_lse[r], (float)whole);
                 stat[buffer][1][row] = s;
             }
         }
@@ -175,7 +178,7 @@ __global__ __launch_bounds__(64 * WAVES, 2) void attention_one_pass_kernel(AttnA
             mine[0] += (float)left;
             mine[entries - 1] += (float)right;
         }
-        bucket_sums<kThreads>(bias.spans, sums, 2 * WAVES, entries, entries, a.table_rows, table_sums(h, part));
+        bucket_sums<kThreads>(bias.spans, sums, 2 * WAVES, entries, entries, a.table_rows, table_sums(h, part), by_p);
         left = right = 0.0;
         __syncthreads();
     };
@@ -315,7 +318,7 @@ __global__ __launch_bounds__(64 * WAVES, 2) void attention_one_pass_kernel(AttnA
             const int i = i0 + 16 * ((wave + WAVES * t) / kWide) + (lane & 15);
             if (wave < kBlocks && i < a.q_len) {
                 T *out = (T *)a.dq.p + ((int64_t)b * a.dq.sb + (int64_t)i * a.dq.st + (int64_t)h * a.dq.sh);
-                const float sc = i < nq ? a.scale : 0.0f;
+                const float sc = i < nq ? a.scale * by_p : 0.0f;
                 store4<T, VEC>(out, 16 * mb + 4 * (lane >> 4), a.dim, x[t][0] * sc, x[t][1] * sc, x[t][2] * sc, x[t][3] * sc);
             }
         }
@@ -348,17 +351,18 @@ __global__ __launch_bounds__(64 * WAVES, 2) void attention_one_pass_kernel(AttnA
     }
     if (parts == 1) {
         const uint32_t room = lds + 32 * wave * tile::kRowBytes;
-        store_rows<T, D, VEC>(dk, a.scale, a.dk, b, hk, jw, a.k_len, a.dim, room, lane);
-        store_rows<T, D, VEC>(dv, 1.0f, a.dv, b, hk, jw, a.k_len, a.dim, room, lane);
+        store_rows<T, D, VEC>(dk, a.scale * by_p, a.dk, b, hk, jw, a.k_len, a.dim, room, lane);
+        store_rows<T, D, VEC>(dv, by_p, a.dv, b, hk, jw, a.k_len, a.dim, room, lane);
     } else if (j < a.k_len) {
+        const float by = a.scale * by_p;
         float *sum = a.part_kv + (((int64_t)part * (a.batch * a.kv_heads - a.whole) + (bh - a.whole)) * a.k_len + j) * (2 * D);
 #pragma unroll
         for (int n = 0; n < D / 32; ++n)
 #pragma unroll
             for (int r = 0; r < 16; r += 4) {
                 const int f = 32 * n + row_of(r, half);
-                *(float4 *)(sum + f) = make_float4(dk[n][r] * a.scale, dk[n][r + 1] * a.scale, dk[n][r + 2] * a.scale, dk[n][r + 3] * a.scale);
-                *(float4 *)(sum + D + f) = make_float4(dv[n][r], dv[n][r + 1], dv[n][r + 2], dv[n][r + 3]);
+                *(float4 *)(sum + f) = make_float4(dk[n][r] * by, dk[n][r + 1] * by, dk[n][r + 2] * by, dk[n][r + 3] * by);
+                *(float4 *)(sum + D + f) = make_float4(dv[n][r] * by_p, dv[n][r + 1] * by_p, dv[n][r + 2] * by_p, dv[n][r + 3] * by_p);
             }
     }
 }

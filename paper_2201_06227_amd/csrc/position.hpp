@@ -114,9 +114,10 @@ __device__ __forceinline__ void each_entry(const Span *spans, int rows, F f)
     }
 }
 
-// What a workgroup makes of sums by distance, copies [copies][stride] in LDS of `entries` each, to the sums by bucket out[0 .. rows).
+// What a workgroup makes of sums by distance, copies [copies][stride] in LDS of `entries` each, to the sums by bucket out[0 .. rows), times
+// `by`.
 template <int THREADS = 256>
-__device__ __forceinline__ void bucket_sums(const Span *spans, float *sums, int copies, int stride, int entries, int rows, float *out)
+__device__ __forceinline__ void bucket_sums(const Span *spans, float *sums, int copies, int stride, int entries, int rows, float *out, float by = 1.0f)
 {
     const int tid = threadIdx.x, lane = tid & 63;
     __syncthreads();
@@ -131,7 +132,7 @@ __device__ __forceinline__ void bucket_sums(const Span *spans, float *sums, int 
         float s = 0.0f;
         for (int e = lane; e < r.count; e += 64) s += sums[r.at + e];
         s = wave_sum(s);
-        if (lane == 0) out[n] = s;
+        if (lane == 0) out[n] = s * by;
     }
 }
 
