@@ -64,15 +64,15 @@ __global__ __launch_bounds__(256, sizeof(T) * row_values(D) == 512 ? 1 : 2) void
     const int qw = q0 + 32 * wave, i = qw + (lane & 31);
     const int64_t row = ((int64_t)b * a.heads + h) * a.q_len + i;
     typename tile::frag q[D / 16], g[D / 16];
-    float delta = 0.0f;
+    double sum = 0.0;                                                       // (a row's error in delta stays in the table's long sums: not one chain of D)
 #pragma unroll
     for (int kk = 0; kk < D / 16; ++kk) {
         q[kk] = qr.frag(qw, kk, lane);
         g[kk] = gr.frag(qw, kk, lane);
-        delta += dot(g[kk], orow.frag(qw, kk, lane));
+        sum += (double)dot(g[kk], orow.frag(qw, kk, lane));
         g[kk] = turned(g[kk], lane);
     }
-    delta += lane_xor<32>(delta);
+    float delta = (float)(sum + __shfl_xor(sum, 32));
     if (half == 0 && i < a.q_len && part == 0) a.delta[row] = delta;
     const float lse = i < nq ? a.lse[row] : -INFINITY;
     // p 2^whole is what the exponential gives; its factor is in the difference that it is multiplied by
