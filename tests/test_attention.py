@@ -452,6 +452,56 @@ def test_attention_repeats_and_captures(eg, dtype):
 
 
 @pytest.mark.gpu
+def test_attention_threads_and_shared_workspaces(eg):
+    """Threads on streams of their own, and captured graphs that share one workspace and are replayed in order: the bits of a single call."""
+    import threading
+    calls = []
+    for n, (dtype, shape, bias) in enumerate((("bf16", (130, 70, 40, 4, 4, 16), (16, 40)), ("bf16", (2, 300, 290, 4, 2, 64), (32, 128)), ("bf16", (1, 1, 5000, 8, 2, 128), None),
+                                              ("f32", (3, 65, 200, 4, 4, 64), (8, 20)))):
+        calls.append(([t.to(DEV) for t in make(dtype, *shape, seed=n)], bias and eg.PositionBias(table(bias[0], shape[3]).to(DEV), bias[1], True)))
+
+    def step(call, ws=None):
+        (q, k, v, dout), pb = call
+        out, lse = eg.attention(q, k, v, causal=True, bias=pb, ws=ws)
+        grads = eg.attention_backward(dout, q, k, v, out, lse, causal=True, bias=pb, ws=ws)
+        return [out, lse, *(g for g in grads if g is not None)]
+
+    want = [step(c) for c in calls]
+    torch.cuda.synchronize()
+    good = [0] * len(calls)
+
+    def work(i):
+        stream = torch.cuda.Stream()
+        with torch.cuda.stream(stream):
+            for _ in range(5):
+                got = step(calls[i])
+                stream.synchronize()
+                good[i] += all(torch.equal(a, b) for a, b in zip(got, want[i]))
+
+    threads = [threading.Thread(target=work, args=(i,)) for i in range(len(calls))]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    assert good == [5] * len(calls)
+    ws = torch.empty(64 << 20, dtype=torch.uint8, device=DEV)
+    held = []
+    for c in calls:
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            out = step(c, ws)
+        held.append((graph, out))
+    for _ in range(3):
+        for _, out in held:
+            for t in out:
+                t.fill_(float("nan"))
+        for graph, _ in held:
+            graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for (_, out), w in zip(held, want) for a, b in zip(out, w))
+
+
+@pytest.mark.gpu
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
 @pytest.mark.parametrize("heads_,nq,nk,offset,buckets,far,both", [
     (1, 1, 1, 0, 2, 2, False), (3, 77, 77, 0, 32, 128, True), (2, 300, 301, 0, 32, 128, True), (2, 301, 2051, 0, 32, 128, False), (4, 33, 500, 467, 20, 50, True),
