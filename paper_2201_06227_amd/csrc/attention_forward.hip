@@ -387,7 +387,8 @@ __global__ __launch_bounds__(256) void attention_join_kernel(AttnArgs a, uint32_
     const int b = (int)(bg / a.kv_heads), g = (int)(bg % a.kv_heads);
     const int head = g * a.group + (int)(row / (uint32_t)a.q_len), qi = (int)(row % (uint32_t)a.q_len);
     const int64_t at = tile * a.splits * kFewRows + n % kFewRows;
-    // eight splits at a time, their statistics and values asked for together
+    // eight splits at a time, their statistics and values asked for together.  A split without a maximum is empty, with sums of 0, or its
+    // scores are NaN, and so are its sums: it is added like any other, against a reference of 0.
     float top = -INFINITY, l = 0.0f, o[4] = {0.0f, 0.0f, 0.0f, 0.0f};
     for (int s0 = 0; s0 < a.splits; s0 += 8) {
         float2 ml[8];
@@ -402,15 +403,14 @@ __global__ __launch_bounds__(256) void attention_join_kernel(AttnArgs a, uint32_
         float to = top;
 #pragma unroll
         for (int s = 0; s < 8; ++s) to = fmaxf(to, ml[s].x);
-        if (to == -INFINITY) continue;
-        const float keep = __builtin_amdgcn_exp2f(top - to);
+        const float base = to == -INFINITY ? 0.0f : to, keep = __builtin_amdgcn_exp2f(top - base);
         l *= keep;
 #pragma unroll
         for (int e = 0; e < 4; ++e) o[e] *= keep;
         top = to;
 #pragma unroll
         for (int s = 0; s < 8; ++s) {
-            const float k = __builtin_amdgcn_exp2f(ml[s].x - top);
+            const float k = __builtin_amdgcn_exp2f(ml[s].x - base);
             l = fmaf(ml[s].y, k, l);
             o[0] = fmaf(x[s].x, k, o[0]);
             o[1] = fmaf(x[s].y, k, o[1]);
