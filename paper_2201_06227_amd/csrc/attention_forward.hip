@@ -388,7 +388,8 @@ __global__ __launch_bounds__(256) void attention_join_kernel(AttnArgs a, uint32_
     const int head = g * a.group + (int)(row / (uint32_t)a.q_len), qi = (int)(row % (uint32_t)a.q_len);
     const int64_t at = tile * a.splits * kFewRows + n % kFewRows;
     // eight splits at a time, their statistics and values asked for together.  A split without a maximum is empty, with sums of 0, or its
-    // scores are NaN, and so are its sums: it is added like any other, against a reference of 0.
+    // scores are NaN, and so are its sums: it is added like any other, against a reference of 0.  What is read in place of a split that
+    // does not exist (finite or not) counts as 0.
     float top = -INFINITY, l = 0.0f, o[4] = {0.0f, 0.0f, 0.0f, 0.0f};
     for (int s0 = 0; s0 < a.splits; s0 += 8) {
         float2 ml[8];
@@ -398,7 +399,10 @@ __global__ __launch_bounds__(256) void attention_join_kernel(AttnArgs a, uint32_
             const int64_t p = at + (int64_t)(s0 + s < a.splits ? s0 + s : s0) * kFewRows;
             ml[s] = *(const float2 *)(a.split_ml + 2 * p);
             x[s] = *(const float4 *)(a.split_o + p * D + f);
-            if (s0 + s >= a.splits) ml[s] = make_float2(-INFINITY, 0.0f);
+            if (s0 + s >= a.splits) {
+                ml[s] = make_float2(-INFINITY, 0.0f);
+                x[s] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+            }
         }
         float to = top;
 #pragma unroll

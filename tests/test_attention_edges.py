@@ -33,3 +33,22 @@ def test_a_query_that_is_nan(eg, dtype, way):  # noqa: F811
     assert torch.isnan(out[b, i, h]).all()
     want["out"][b, i, h], out[b, i, h] = 0.0, 0.0
     close(out, want["out"], want["bound"]["out"], way)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("way", WAYS)
+@pytest.mark.parametrize("at", [0, 0.5, 1])
+def test_a_value_that_is_not_finite(eg, dtype, way, at):  # noqa: F811
+    """Every query that sees it has it in its feature, with its sign, and nowhere else."""
+    q, k, v, _ = make(dtype, *WAYS[way], seed=22)
+    want = clean(dtype, q, k, v)["out"]
+    j, g, group = int(at * (k.shape[1] - 1)), v.shape[2] - 1, q.shape[2] // v.shape[2]
+    rows = (0, slice(None), slice(g * group, (g + 1) * group))
+    for x in (math.inf, -math.inf, math.nan):
+        v[0, j, g, 7] = x
+        out, _ = eg.attention(q.to(DEV), k.to(DEV), v.to(DEV))
+        got = np64(out)
+        assert np.array_equal(got[rows][..., 7], np.full_like(want[rows][..., 7], x), equal_nan=True), x
+        got[rows][..., 7] = 0.0
+        assert np.isfinite(got).all(), x
