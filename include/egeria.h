@@ -499,8 +499,9 @@ egeria_status egeria_cache_get(const egeria_cache_desc *desc, const void *cache,
  * A row without a visible pair (an empty sequence, a query beyond n_q, a causal
  * query before the first key) has o = 0 and L = -infinity.  Keys and values at
  * or beyond n_k, and queries at or beyond n_q, may hold anything; a non-finite
- * value of a key below n_k may reach every query of its sequence, as in any
- * product.
+ * value of a key below n_k may reach every query of its sequence, and one of a
+ * query or of dout below n_q every key's gradient, as in any product.  A row
+ * with a score that is NaN or +infinity has L = NaN.
  * Backward, from dout = dLoss/do:
  *   D_i = <dout_i, o_i>,  ds_ij = p_ij (<dout_i, v_j> - D_i)
  *   dq_i = scale sum_j ds_ij k_j,  dk_j = scale sum_{i, h of group g} ds_ij q_i,

@@ -93,6 +93,10 @@ __device__ __forceinline__ float largest(const v16f (&s)[N])
     return top;
 }
 
+// L of a row from its reference and its sum against that: minus infinity if nothing was added; NaN, from a score that is NaN or
+// infinite, stays
+__device__ __forceinline__ float log_sum(float m, float l) { return l == 0.0f ? -INFINITY : (m + __builtin_amdgcn_logf(l)) * kLn2; }
+
 template <typename T, int D, bool VEC>
 __global__ __launch_bounds__(256, sizeof(T) * row_values(D) == 512 ? 1 : 2) void attention_forward_kernel(AttnArgs a)
 {
@@ -194,7 +198,7 @@ __global__ __launch_bounds__(256, sizeof(T) * row_values(D) == 512 ? 1 : 2) void
 
     const float total = st.l + lane_xor<32>(st.l), l = i < nq ? total : 0.0f;
     if (half == 0 && i < a.q_len)
-        a.lse[((int64_t)b * a.heads + h) * a.q_len + i] = l > 0.0f ? (st.m + __builtin_amdgcn_logf(l)) * kLn2 : -INFINITY;
+        a.lse[((int64_t)b * a.heads + h) * a.q_len + i] = log_sum(st.m, l);
     __syncthreads();                                                        // the tiles have been read
     store_rows<T, D, VEC>(st.o, l > 0.0f ? 1.0f / l : 0.0f, a.o, b, h, qw, a.q_len, a.dim, lds + 32 * wave * tile::kRowBytes, lane);
 }
@@ -359,7 +363,7 @@ __global__ __launch_bounds__(256) void attention_few_kernel(AttnArgs a)
             const float inv = l > 0.0f ? 1.0f / l : 0.0f;
             T *out = (T *)a.o.p + ((int64_t)b * a.o.sb + (int64_t)qi * a.o.st + (int64_t)head * a.o.sh);
             store4<T, VEC>(out, f, a.dim, o[0] * inv, o[1] * inv, o[2] * inv, o[3] * inv);
-            if (f == 0) a.lse[((int64_t)b * a.heads + head) * a.q_len + qi] = l > 0.0f ? (top + __builtin_amdgcn_logf(l)) * kLn2 : -INFINITY;
+            if (f == 0) a.lse[((int64_t)b * a.heads + head) * a.q_len + qi] = log_sum(top, l);
         } else {
             const int64_t at = ((((int64_t)b * a.kv_heads + g) * tiles + rt) * a.splits + split) * kFewRows + row;
             *(float4 *)(a.split_o + at * D + f) = make_float4(o[0], o[1], o[2], o[3]);
@@ -426,7 +430,7 @@ __global__ __launch_bounds__(256) void attention_join_kernel(AttnArgs a, uint32_
     const float inv = l > 0.0f ? 1.0f / l : 0.0f;
     T *out = (T *)a.o.p + ((int64_t)b * a.o.sb + (int64_t)qi * a.o.st + (int64_t)head * a.o.sh);
     store4<T, VEC>(out, f, a.dim, o[0] * inv, o[1] * inv, o[2] * inv, o[3] * inv);
-    if (f == 0) a.lse[((int64_t)b * a.heads + head) * a.q_len + qi] = l > 0.0f ? (top + __builtin_amdgcn_logf(l)) * kLn2 : -INFINITY;
+    if (f == 0) a.lse[((int64_t)b * a.heads + head) * a.q_len + qi] = log_sum(top, l);
 }
 
 template <typename T, int D, bool VEC>

@@ -52,3 +52,59 @@ def test_a_value_that_is_not_finite(eg, dtype, way, at):  # noqa: F811
         assert np.array_equal(got[rows][..., 7], np.full_like(want[rows][..., 7], x), equal_nan=True), x
         got[rows][..., 7] = 0.0
         assert np.isfinite(got).all(), x
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("way", WAYS)
+def test_log_sum_exp_of_scores_that_are_not_finite(eg, dtype, way):  # noqa: F811
+    """NaN where a score is NaN or overflows; minus infinity is that of a row without a visible pair."""
+    q, k, v, _ = make(dtype, *WAYS[way], seed=23)
+    lens = [k.shape[1]] * (q.shape[0] - 1) + [0 if q.shape[0] > 1 else k.shape[1]]
+    kl = torch.tensor(lens, dtype=torch.int32, device=DEV)
+    want = clean(dtype, q, k, v, k_lens=lens)
+    group, j = q.shape[2] // k.shape[2], k.shape[1] // 2
+    nan_q, nan_k, big_q, big_k = q.clone(), k.clone(), q.clone(), k.clone()
+    nan_q[0, 0, 1, 3] = math.nan
+    nan_k[0, j, 1, 3] = math.nan
+    big_q[0, 0, group, 3], big_k[0, j, 1, 3] = 2.0 ** 70, 2.0 ** 70     # of head `group`, the first of key head 1
+    big_q[0, :, group + 1:2 * group, 3] = 0.0
+    big_q[0, 1:, group, 3] = 0.0
+    for what, (qq, kk), rows in (("query", (nan_q, k), (0, 1, 0)), ("key", (q, nan_k), (0, slice(group, 2 * group))), ("overflow", (big_q, big_k), (0, group, 0))):
+        out, lse = eg.attention(qq.to(DEV), kk.to(DEV), v.to(DEV), k_lens=kl)
+        assert torch.isnan(lse[rows]).all() and torch.isnan(out.transpose(1, 2)[rows]).all(), what
+        if what != "overflow":                                 # (there the other rows are others too)
+            lse[rows] = 0.0
+            exp = want["lse"].copy()
+            exp[rows] = 0.0
+            close(lse, exp, want["bound"]["lse"], what)
+        else:
+            assert torch.isnan(lse).sum() == 1
+        if lens[-1] == 0:
+            assert torch.isneginf(lse[-1]).all() and not out[-1].any()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("shape", [(2, 70, 150, 4, 2, 64), (1, 150, 300, 4, 2, 128), (64, 20, 40, 4, 2, 32), (64, 70, 200, 4, 2, 64)], ids=str)
+def test_gradients_of_a_query_that_is_nan(eg, dtype, shape):  # noqa: F811
+    """Its own gradient, those of the keys and values it sees and of its head's table are NaN; everything else is as without it."""
+    q, k, v, dout = make(dtype, *shape, seed=24)
+    b, i, h, g = shape[0] - 1, 11, 3, 1
+    tab = torch.randn(8, 4, generator=torch.Generator().manual_seed(1))
+    q[b, i, h, 2] = math.nan
+    on = [t.to(DEV) for t in (q, k, v)]
+    pb = eg.PositionBias(tab.to(DEV), 20, True)
+    out, lse = eg.attention(*on, bias=pb)
+    dq, dk, dv, dtable = eg.attention_backward(dout.to(DEV), *on, out, lse, bias=pb)
+    assert torch.isnan(dq[b, i, h]).all() and torch.isnan(dk[b, :, g]).all() and torch.isnan(dv[b, :, g]).all()
+    assert torch.isnan(dtable[[n for n in range(8) if n != 4], h]).all()        # (row 4 would be distance 0 of the later keys, which the earlier ones have)
+    saved, h_out, h_op = (np64(out), np64(lse)), *STEPS[dtype]
+    saved[0][b, i, h], saved[1][b, h, i] = 0.0, -math.inf
+    q[b, i, h, 2] = 0.0
+    want = ao.attention(np64(q), np64(k), np64(v), np.float64(np.float32(1.0 / math.sqrt(shape[5]))), bias=(np64(tab), 20, True), dout=np64(dout), saved=saved,
+                        half_step=h_out, operand_step=h_op)
+    for name, t, at in (("dq", dq, (b, i, h)), ("dk", dk, (b, slice(None), g)), ("dv", dv, (b, slice(None), g)), ("dtable", dtable, (slice(None), h))):
+        t[at] = 0.0
+        want[name][at] = 0.0
+        close(t, want[name], want["bound"][name], name)
