@@ -150,7 +150,11 @@ __global__ __launch_bounds__(256, sizeof(T) * row_values(D) == 512 ? 1 : 2) void
         if (step + 1 < steps) one_step(Const<1>(), step + 1);
     }
 
-    const float by = i < nq ? a.scale : 0.0f;
+    const float by = a.scale;
+    if (lse == -INFINITY) {                                                 // (a row without a pair: 0 times a difference that is not finite is no zero)
+#pragma unroll
+        for (int n = 0; n < D / 32; ++n) dq[n] = v16f(0.0f);
+    }
     __syncthreads();                                                        // the tiles have been read
     if (a.q_parts == 1) store_rows<T, D, VEC>(dq, by, a.dq, b, h, qw, a.q_len, a.dim, lds + 32 * wave * tile::kRowBytes, lane);
     else if (i < a.q_len) {

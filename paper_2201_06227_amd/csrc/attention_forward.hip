@@ -93,6 +93,16 @@ __device__ __forceinline__ float largest(const v16f (&s)[N])
     return top;
 }
 
+// Four features of a row: its sums over the sum of its weights, zeros if nothing was added (whatever was taken 0 times)
+template <typename T, bool VEC>
+__device__ __forceinline__ void store_row(const AttnArgs &a, int b, int i, int h, int f, const float (&o)[4], float l)
+{
+    const float inv = 1.0f / l;
+    float x[4];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) x[e] = l == 0.0f ? 0.0f : o[e] * inv;
+    store4<T, VEC>((T *)a.o.p + ((int64_t)b * a.o.sb + (int64_t)i * a.o.st + (int64_t)h * a.o.sh), f, a.dim, x[0], x[1], x[2], x[3]);
+}
 // L of a row from its reference and its sum against that: minus infinity if nothing was added; NaN, from a score that is NaN or
 // infinite, stays
 __device__ __forceinline__ float log_sum(float m, float l) { return l == 0.0f ? -INFINITY : (m + __builtin_amdgcn_logf(l)) * kLn2; }
@@ -200,7 +210,11 @@ __global__ __launch_bounds__(256, sizeof(T) * row_values(D) == 512 ? 1 : 2) void
     if (half == 0 && i < a.q_len)
         a.lse[((int64_t)b * a.heads + h) * a.q_len + i] = log_sum(st.m, l);
     __syncthreads();                                                        // the tiles have been read
-    store_rows<T, D, VEC>(st.o, l > 0.0f ? 1.0f / l : 0.0f, a.o, b, h, qw, a.q_len, a.dim, lds + 32 * wave * tile::kRowBytes, lane);
+    if (l == 0.0f) {                                                        // (a weight of 0 does not make zeros of values that are not finite)
+#pragma unroll
+        for (int n = 0; n < D / 32; ++n) st.o[n] = v16f(0.0f);
+    }
+    store_rows<T, D, VEC>(st.o, l == 0.0f ? 0.0f : 1.0f / l, a.o, b, h, qw, a.q_len, a.dim, lds + 32 * wave * tile::kRowBytes, lane);
 }
 
 // ---- few rows ---------------------------------------------------------------------------------------------------
@@ -360,9 +374,7 @@ __global__ __launch_bounds__(256) void attention_few_kernel(AttnArgs a)
         const int head = g * a.group + (int)((r0 + row) / (uint32_t)a.q_len), qi = (int)((r0 + row) % (uint32_t)a.q_len);
         if (a.splits == 1) {
             if (qi >= nq) l = 0.0f;
-            const float inv = l > 0.0f ? 1.0f / l : 0.0f;
-            T *out = (T *)a.o.p + ((int64_t)b * a.o.sb + (int64_t)qi * a.o.st + (int64_t)head * a.o.sh);
-            store4<T, VEC>(out, f, a.dim, o[0] * inv, o[1] * inv, o[2] * inv, o[3] * inv);
+            store_row<T, VEC>(a, b, qi, head, f, o, l);
             if (f == 0) a.lse[((int64_t)b * a.heads + head) * a.q_len + qi] = log_sum(top, l);
         } else {
             const int64_t at = ((((int64_t)b * a.kv_heads + g) * tiles + rt) * a.splits + split) * kFewRows + row;
@@ -427,9 +439,7 @@ __global__ __launch_bounds__(256) void attention_join_kernel(AttnArgs a, uint32_
         }
     }
     if (qi >= clamped(a.q_lens, b, a.q_len)) l = 0.0f;
-    const float inv = l > 0.0f ? 1.0f / l : 0.0f;
-    T *out = (T *)a.o.p + ((int64_t)b * a.o.sb + (int64_t)qi * a.o.st + (int64_t)head * a.o.sh);
-    store4<T, VEC>(out, f, a.dim, o[0] * inv, o[1] * inv, o[2] * inv, o[3] * inv);
+    store_row<T, VEC>(a, b, qi, head, f, o, l);
     if (f == 0) a.lse[((int64_t)b * a.heads + head) * a.q_len + qi] = log_sum(top, l);
 }
 

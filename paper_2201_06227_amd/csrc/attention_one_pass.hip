@@ -291,8 +291,9 @@ __global__ __launch_bounds__(64 * WAVES, 2) void attention_one_pass_kernel(AttnA
         __syncthreads();
         // dQ^T of the step, 16 features of 16 queries at a time, over all keys: a wave's blocks have the same features, so they share
         // the keys' fragments; several chunks of keys are read ahead of their products (one at a time the waits for LDS made this 1.5 us
-        // of a step's 5)
-        constexpr int kWide = D / 16, kBlocks = kWide * (kQueries / 16), kMine = kBlocks > WAVES ? kBlocks / WAVES : 1, kAhead = 4;
+        // of a step's 5).  bf16 in workgroups of four waves, which have twice the blocks each: two, since with four a wave's registers
+        // overflow (200 x 128 x 8 x 64 82 us, now 65).
+        constexpr int kWide = D / 16, kBlocks = kWide * (kQueries / 16), kMine = kBlocks > WAVES ? kBlocks / WAVES : 1, kAhead = sizeof(T) == 2 && WAVES == 4 ? 2 : 4;
         const int mb = wave % kWide;
         v4f x[kMine];
 #pragma unroll
@@ -316,9 +317,9 @@ __global__ __launch_bounds__(64 * WAVES, 2) void attention_one_pass_kernel(AttnA
 #pragma unroll
         for (int t = 0; t < kMine; ++t) {
             const int i = i0 + 16 * ((wave + WAVES * t) / kWide) + (lane & 15);
-            if (wave < kBlocks && i < a.q_len) {
+            if (wave < kBlocks && i < nq && i + shift >= 0) {
                 T *out = (T *)a.dq.p + ((int64_t)b * a.dq.sb + (int64_t)i * a.dq.st + (int64_t)h * a.dq.sh);
-                const float sc = i < nq ? a.scale * by_p : 0.0f;
+                const float sc = a.scale * by_p;
                 store4<T, VEC>(out, 16 * mb + 4 * (lane >> 4), a.dim, x[t][0] * sc, x[t][1] * sc, x[t][2] * sc, x[t][3] * sc);
             }
         }
@@ -338,10 +339,11 @@ __global__ __launch_bounds__(64 * WAVES, 2) void attention_one_pass_kernel(AttnA
                 if (q != part || h < seen0 || h >= seen1) table_sums(h, q)[n % a.table_rows] = 0.0f;
         }
     }
-    // queries behind the last step
-    const int done = per_head * kQueries, rest = a.q_len - done;
-    for (int64_t n = tid; part == 0 && n < (int64_t)rest * a.group * (D / 4); n += kThreads) {
-        const int f = (int)(n % (D / 4)) * 4, h = hk * a.group + (int)(n / (D / 4) % a.group), i = done + (int)(n / (D / 4) / a.group);
+    // dq of queries that see no key, which in a step would be sums of 0 times anything
+    const int live1 = nk > 0 ? nq : 0, live0 = shift < 0 && nk > 0 ? -shift : 0, none = a.q_len - (live1 - live0);
+    for (int64_t n = tid; part == 0 && n < (int64_t)none * a.group * (D / 4); n += kThreads) {
+        const int f = (int)(n % (D / 4)) * 4, h = hk * a.group + (int)(n / (D / 4) % a.group), m = (int)(n / (D / 4) / a.group);
+        const int i = m < live0 ? m : m + (live1 - live0);
         store4<T, VEC>((T *)a.dq.p + ((int64_t)b * a.dq.sb + (int64_t)i * a.dq.st + (int64_t)h * a.dq.sh), f, a.dim, 0.0f, 0.0f, 0.0f, 0.0f);
     }
     __syncthreads();                                                        // the keys have been read

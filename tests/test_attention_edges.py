@@ -108,3 +108,27 @@ def test_gradients_of_a_query_that_is_nan(eg, dtype, shape):  # noqa: F811
         t[at] = 0.0
         want[name][at] = 0.0
         close(t, want[name], want["bound"][name], name)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("x", [math.nan, math.inf])
+@pytest.mark.parametrize("shape", [(2, 20, 200, 4, 2, 64), (2, 9, 900, 4, 2, 64), (4, 130, 200, 12, 4, 64), (64, 70, 40, 4, 2, 64), (33, 100, 200, 4, 4, 33)], ids=str)
+def test_rows_without_a_pair_are_zero_beside_values_that_are_not_finite(eg, dtype, x, shape):  # noqa: F811
+    """Queries behind their sequence, and causal ones before its first key: zeros in out and dq, whatever the keys and values of their sequence hold."""
+    nq, nk = shape[1], shape[2]
+    tab = eg.PositionBias(torch.randn(8, shape[3], generator=torch.Generator().manual_seed(2)).to(DEV), 20, True)
+    for causal, ql, kl in ((False, nq - 3, nk - 5), (True, nq - 3, nk - 5), (True, nq - 1, 4), (True, nq, 1)):
+        q, k, v, dout = (t.to(DEV) for t in make(dtype, *shape, seed=25))
+        k[0, 0, 0, 1] = v[0, 0, 1, 1] = x
+        lens = [torch.full((shape[0],), n, dtype=torch.int32, device=DEV) for n in (ql, kl)]
+        none = [i for i in range(nq) if i >= ql or (causal and i + kl - ql < 0)]
+        for pb in (None, tab):
+            how = dict(causal=causal, q_lens=lens[0], k_lens=lens[1], bias=pb)
+            out, lse = eg.attention(q, k, v, **how)
+            dq, dk, dv, _ = eg.attention_backward(dout, q, k, v, out, lse, **how)
+            what = (causal, ql, kl, pb is not None)
+            assert (out[:, none] == 0).all() and torch.isneginf(lse[:, :, none]).all(), what
+            assert (dq[:, none] == 0).all(), what
+            assert (dk[:, kl:] == 0).all() and (dv[:, kl:] == 0).all(), what
+            assert torch.isfinite(out[1:]).all() and all(torch.isfinite(t[1:]).all() for t in (dq, dk, dv)), what
