@@ -751,6 +751,15 @@ def _same_device(*tensors: Optional[torch.Tensor]) -> int:
     return dev
 
 
+def _no_graph(*tensors: Optional[torch.Tensor]):
+    """The calls below record nothing for autograd: a tensor that wants a gradient through them would silently get none."""
+    if torch.is_grad_enabled():
+        for t in tensors:
+            if t is not None and t.requires_grad:
+                raise ValueError("a result would have no autograd graph: call this under torch.no_grad() or with detached tensors "
+                                 "(the gradient is attention_backward's, position_bias_backward's)")
+
+
 def _heads(t: torch.Tensor) -> bytes:
     """egeria_heads of a tensor [batch, token, head, feature]."""
     if t.dim() != 4:
@@ -810,7 +819,8 @@ def attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, causal: bool = 
               ws: Optional[torch.Tensor] = None):
     """egeria_attention: q [batch, q_len, heads, dim], k and v [batch, k_len, kv_heads, dim] (any strides with contiguous
     features) -> out like q, and lse fp32 [batch, heads, q_len].  scale: 1 / sqrt(dim) if not given.  No autograd: the gradient is
-    attention_backward's."""
+    attention_backward's, and tensors that require one are refused unless in torch.no_grad()."""
+    _no_graph(q, k, v, None if bias is None else bias.table)
     dev = _same_device(q, k, v, q_lens, k_lens, out, lse, ws, None if bias is None else bias.table)
     desc, sizes, _tab = _attention_desc(q, k, v, causal, scale, q_lens, k_lens, bias)
     batch, q_len, heads, _ = q.shape
@@ -838,7 +848,8 @@ def attention_backward(dout: torch.Tensor, q: torch.Tensor, k: torch.Tensor, v: 
                        ws: Optional[torch.Tensor] = None, table_grad: bool = True):
     """egeria_attention_backward: (dq, dk, dv, dtable) from the arguments and results of attention().  dtable is fp32
     [buckets, heads], or None without bias or with table_grad = False.  dq, dk, dv: tensors to write, e.g. the slices of a packed
-    gradient."""
+    gradient.  No gradient of the gradient: a dout that requires one is refused unless in torch.no_grad()."""
+    _no_graph(dout)
     dev = _same_device(dout, q, k, v, out, lse, q_lens, k_lens, dq, dk, dv, ws, None if bias is None else bias.table)
     desc, sizes, _tab = _attention_desc(q, k, v, causal, scale, q_lens, k_lens, bias)
     if dout.shape != q.shape or dout.dtype != q.dtype or out.shape != q.shape or out.dtype != q.dtype:
@@ -866,7 +877,9 @@ def attention_backward(dout: torch.Tensor, q: torch.Tensor, k: torch.Tensor, v: 
 
 def position_bias(bias: PositionBias, q_len: int, k_len: int, offset: int = 0, dtype: torch.dtype = torch.float32,
                   out: Optional[torch.Tensor] = None) -> torch.Tensor:
-    """egeria_position_bias: [heads, q_len, k_len] of table entries; offset = position of query 0 among the keys."""
+    """egeria_position_bias: [heads, q_len, k_len] of table entries; offset = position of query 0 among the keys.  A table that
+    requires a gradient is refused unless in torch.no_grad()."""
+    _no_graph(bias.table)
     _same_device(bias.table, out)
     tab, heads = bias.c_struct(), bias.table.shape[1]
     if out is None:
@@ -881,6 +894,7 @@ def position_bias(bias: PositionBias, q_len: int, k_len: int, offset: int = 0, d
 def position_bias_backward(dbias: torch.Tensor, bias: PositionBias, offset: int = 0, ws: Optional[torch.Tensor] = None) -> torch.Tensor:
     """egeria_position_bias_backward: the gradient [buckets, heads] of bias.table from dbias [batch, heads, q_len, k_len] (or
     [heads, q_len, k_len])."""
+    _no_graph(dbias)
     _same_device(dbias, bias.table, ws)
     tab, heads = bias.c_struct(), bias.table.shape[1]
     if dbias.dim() not in (3, 4) or dbias.shape[-3] != heads:

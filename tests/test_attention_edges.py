@@ -132,3 +132,44 @@ def test_rows_without_a_pair_are_zero_beside_values_that_are_not_finite(eg, dtyp
             assert (dq[:, none] == 0).all(), what
             assert (dk[:, kl:] == 0).all() and (dv[:, kl:] == 0).all(), what
             assert torch.isfinite(out[1:]).all() and all(torch.isfinite(t[1:]).all() for t in (dq, dk, dv)), what
+
+
+def test_no_silent_loss_of_a_graph(eg):  # noqa: F811
+    """The calls record nothing for autograd, so they refuse tensors that want a gradient through them (before anything else: on the host)."""
+    x, tab = torch.zeros(1, 2, 2, 8), torch.zeros(8, 2)
+    want, bias = x.clone().requires_grad_(), eg.PositionBias(tab.clone().requires_grad_(), 20)
+    calls = [lambda: eg.attention(want, x, x), lambda: eg.attention(x, want, x), lambda: eg.attention(x, x, want), lambda: eg.attention(x, x, x, bias=bias),
+             lambda: eg.attention_backward(want, x, x, x, x, x), lambda: eg.position_bias(bias, 4, 4),
+             lambda: eg.position_bias_backward(torch.zeros(1, 2, 4, 4, requires_grad=True), eg.PositionBias(tab, 20))]
+    for call in calls:
+        with pytest.raises(ValueError, match="autograd"):
+            call()
+        with torch.no_grad(), pytest.raises(ValueError, match="device"):       # (host tensors)
+            call()
+    with pytest.raises(ValueError, match="device"):                            # what a hand-written backward pass has saved may require one
+        eg.attention_backward(x, want, want, want, want, x, bias=bias)
+
+
+@pytest.mark.gpu
+def test_calls_of_an_autograd_function(eg):  # noqa: F811
+    """In a torch.autograd.Function, where there is no graph, leaves may require gradients; they get those of the formula."""
+    q, k, v, dout = (t.to(DEV) for t in make("f32", 2, 20, 30, 4, 2, 16, seed=31))
+    tab = torch.randn(8, 4, generator=torch.Generator().manual_seed(3)).to(DEV)
+
+    class Attention(torch.autograd.Function):
+        @staticmethod
+        def forward(ctx, q, k, v, tab):
+            out, lse = eg.attention(q, k, v, bias=eg.PositionBias(tab, 20))
+            ctx.save_for_backward(q, k, v, tab, out, lse)
+            return out
+
+        @staticmethod
+        def backward(ctx, dout):
+            q, k, v, tab, out, lse = ctx.saved_tensors
+            return eg.attention_backward(dout, q, k, v, out, lse, bias=eg.PositionBias(tab, 20))
+
+    leaves = [t.clone().requires_grad_() for t in (q, k, v, tab)]
+    Attention.apply(*leaves).backward(dout)
+    out, lse = eg.attention(q, k, v, bias=eg.PositionBias(tab, 20))
+    for leaf, g in zip(leaves, eg.attention_backward(dout, q, k, v, out, lse, bias=eg.PositionBias(tab, 20))):
+        assert torch.equal(leaf.grad, g)
