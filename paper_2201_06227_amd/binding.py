@@ -721,7 +721,7 @@ class PositionBias(NamedTuple):
         t = _dev(self.table)
         if t.dtype != torch.float32 or t.dim() != 2:
             raise ValueError("a position table is fp32 [buckets, heads]")
-        return PositionTable(t.data_ptr(), t.shape[0], _int32(self.max_distance), 1 if self.bidirectional else 0)
+        return PositionTable(t.data_ptr(), _int32(t.shape[0]), _int32(self.max_distance), 1 if self.bidirectional else 0)
 
 
 # The calls below are short beside the host's work for them, which is all of a small call's time: descriptors are packed as bytes
@@ -899,7 +899,7 @@ def position_bias_backward(dbias: torch.Tensor, bias: PositionBias, offset: int 
     tab, heads = bias.c_struct(), bias.table.shape[1]
     if dbias.dim() not in (3, 4) or dbias.shape[-3] != heads:
         raise ValueError("dbias must be [batch, heads, q_len, k_len]")
-    batch, q_len, k_len = dbias.shape[0] if dbias.dim() == 4 else 1, dbias.shape[-2], dbias.shape[-1]
+    batch, q_len, k_len = (_int32(n) for n in (dbias.shape[0] if dbias.dim() == 4 else 1, *dbias.shape[-2:]))
     dtable = torch.empty_like(bias.table)
     if ws is None:
         ws = workspace(int(lib().egeria_position_bias_workspace_bytes(tab, batch, heads, q_len, k_len, _dt(dbias))), dbias.device)

@@ -173,3 +173,14 @@ def test_calls_of_an_autograd_function(eg):  # noqa: F811
     out, lse = eg.attention(q, k, v, bias=eg.PositionBias(tab, 20))
     for leaf, g in zip(leaves, eg.attention_backward(dout, q, k, v, out, lse, bias=eg.PositionBias(tab, 20))):
         assert torch.equal(leaf.grad, g)
+
+
+@pytest.mark.parametrize("shape", [(1, 2, (1 << 32) + 4, 1), ((1 << 32) + 2, 2, 1, 1), (1, 2, 1, (1 << 32) + 1)])
+def test_sizes_beyond_c(eg, monkeypatch, shape):  # noqa: F811
+    """A bias gradient with a size that a C int does not hold is refused, not taken for the size that is left of it (tensors without memory)."""
+    monkeypatch.setattr(eg, "_same_device", lambda *t: 0)
+    monkeypatch.setattr(eg, "_dev", lambda t: t)
+    with pytest.raises(ValueError, match="out of range"):
+        eg.position_bias_backward(torch.empty(shape, device="meta"), eg.PositionBias(torch.zeros(8, 2), 20))
+    with pytest.raises(ValueError, match="out of range"):
+        eg.PositionBias(torch.empty((1 << 32) + 8, 1, device="meta"), 20).c_struct()
