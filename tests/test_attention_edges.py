@@ -7,7 +7,7 @@ import pytest
 import torch
 
 from oracle import attention_oracle as ao
-from test_attention import DEV, STEPS, T, close, eg, make, np64  # noqa: F401  (eg: the fixture)
+from test_attention import DEV, STEPS, T, close, eg, make, np64, run_and_check  # noqa: F401  (eg: the fixture)
 
 # A call for each way through the forward pass: a workgroup of four waves for a few rows with one, four and twenty workgroups to
 # share the keys, and tiles of 128 queries (at least 48 of them).  batch, q_len, k_len, heads, kv_heads, dim
@@ -184,3 +184,13 @@ def test_sizes_beyond_c(eg, monkeypatch, shape):  # noqa: F811
         eg.position_bias_backward(torch.empty(shape, device="meta"), eg.PositionBias(torch.zeros(8, 2), 20))
     with pytest.raises(ValueError, match="out of range"):
         eg.PositionBias(torch.empty((1 << 32) + 8, 1, device="meta"), 20).c_struct()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("strides", [(40, 1, 20, 1), (40, 8, 1, 1), (0, 1, 0, 1), (0, 0, 0, 1)], ids=str)
+def test_inputs_whose_elements_overlap(eg, dtype, strides):  # noqa: F811
+    """Windows of one run of values, broadcast heads, tokens and sequences: any strides whose features are contiguous."""
+    shape = (2, 3, 2, 8)
+    x = torch.randn(4, 100, generator=torch.Generator().manual_seed(5)).to(T[dtype]).to(DEV)
+    run_and_check(eg, dtype, *(r.as_strided(shape, strides) for r in x))
