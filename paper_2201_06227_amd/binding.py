@@ -819,6 +819,13 @@ def _attention_workspace_bytes(desc: bytes, sizes: tuple, backward: int) -> int:
     return n
 
 
+def _room(ws: torch.Tensor) -> int:
+    """Bytes of a workspace of uint8"""
+    if not ws.is_contiguous():
+        raise ValueError("a contiguous workspace expected")
+    return ws.numel()
+
+
 def attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, causal: bool = False, scale: Optional[float] = None,
               q_lens: Optional[torch.Tensor] = None, k_lens: Optional[torch.Tensor] = None,
               bias: Optional[PositionBias] = None, out: Optional[torch.Tensor] = None, lse: Optional[torch.Tensor] = None,
@@ -840,7 +847,7 @@ def attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, causal: bool = 
         raise ValueError("lse must be a contiguous fp32 tensor [batch, heads, q_len]")
     if ws is None:
         ws = torch.empty(_attention_workspace_bytes(desc, sizes, 0), dtype=torch.uint8, device=q.device)
-    rc = _raw("egeria_attention", 9)(desc, _heads(q), _heads(k), _heads(v), _heads(out), lse.data_ptr(), ws.data_ptr(), ws.numel(),
+    rc = _raw("egeria_attention", 9)(desc, _heads(q), _heads(k), _heads(v), _heads(out), lse.data_ptr(), ws.data_ptr(), _room(ws),
                                      torch._C._cuda_getCurrentRawStream(dev))
     if rc:
         _check(rc, "egeria_attention")
@@ -875,7 +882,7 @@ def attention_backward(dout: torch.Tensor, q: torch.Tensor, k: torch.Tensor, v: 
         ws = torch.empty(_attention_workspace_bytes(desc, sizes, 1), dtype=torch.uint8, device=q.device)
     rc = _raw("egeria_attention_backward", 14)(
         desc, _heads(dout), _heads(q), _heads(k), _heads(v), _heads(out), lse.data_ptr(), _heads(grads[0]), _heads(grads[1]),
-        _heads(grads[2]), None if dtable is None else dtable.data_ptr(), ws.data_ptr(), ws.numel(), torch._C._cuda_getCurrentRawStream(dev))
+        _heads(grads[2]), None if dtable is None else dtable.data_ptr(), ws.data_ptr(), _room(ws), torch._C._cuda_getCurrentRawStream(dev))
     if rc:
         _check(rc, "egeria_attention_backward")
     return (*grads, dtable)
@@ -910,7 +917,7 @@ def position_bias_backward(dbias: torch.Tensor, bias: PositionBias, offset: int 
     if ws is None:
         ws = workspace(int(lib().egeria_position_bias_workspace_bytes(tab, batch, heads, q_len, k_len, _dt(dbias))), dbias.device)
     rc = lib().egeria_position_bias_backward(tab, _ptr(_dev(dbias)), _dt(dbias), batch, heads, q_len, k_len, _int32(offset),
-                                             _ptr(dtable), _ptr(ws), ws.numel(), _stream())
+                                             _ptr(dtable), _ptr(ws), _room(ws), _stream())
     _check(rc, "egeria_position_bias_backward")
     return dtable
 

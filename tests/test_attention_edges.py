@@ -194,3 +194,16 @@ def test_inputs_whose_elements_overlap(eg, dtype, strides):  # noqa: F811
     shape = (2, 3, 2, 8)
     x = torch.randn(4, 100, generator=torch.Generator().manual_seed(5)).to(T[dtype]).to(DEV)
     run_and_check(eg, dtype, *(r.as_strided(shape, strides) for r in x))
+
+
+def test_workspaces_that_are_smaller_than_they_look(eg, monkeypatch):  # noqa: F811
+    """A workspace whose elements lie on each other has fewer bytes than elements: refused on the host (where these tensors are)."""
+    monkeypatch.setattr(eg, "_same_device", lambda *t: 0)
+    monkeypatch.setattr(eg, "_dev", lambda t: t)
+    monkeypatch.setattr(torch._C, "_cuda_getCurrentRawStream", lambda dev: 0, raising=False)
+    monkeypatch.setattr(eg, "_stream", lambda: 0)
+    x, ws, pb = torch.zeros(1, 2, 2, 8), torch.zeros(256, dtype=torch.uint8)[:1].expand(1 << 20), eg.PositionBias(torch.zeros(8, 2), 20)
+    lse = torch.zeros(1, 2, 2)
+    for call in (lambda: eg.attention(x, x, x, ws=ws), lambda: eg.attention_backward(x, x, x, x, x, lse, ws=ws), lambda: eg.position_bias_backward(torch.zeros(1, 2, 4, 4), pb, ws=ws)):
+        with pytest.raises(ValueError, match="workspace"):
+            call()
