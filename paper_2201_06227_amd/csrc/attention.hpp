@@ -214,9 +214,11 @@ __device__ __forceinline__ int row_of(int r, int half) { return 8 * (r >> 2) + 4
 // if turn() takes different values over the rows that share a place; and of the four rows that half a wave reads 4 units of each
 // across, those that share places have turn() differ in the bits above the lowest two.  Rows of 128 bytes (two to a line of banks): the
 // bits of r / 2 in reverse; longer rows: r with its lowest two bits on top.
+constexpr int kTileAlign = 512;             // of LDS that holds tiles: a whole number of rows (Lane)
 template <typename T, int D>
 struct Tile {
     static constexpr int kUnits = D * (int)sizeof(T) / 16, kRowBytes = D * (int)sizeof(T);
+    static_assert(kTileAlign % kRowBytes == 0, "bits of a unit are changed in an address");
     static __device__ __forceinline__ int turn(int r)
     {
         if constexpr (kUnits == 8) return ((r >> 1) & 1) << 2 | ((r >> 2) & 1) << 1 | ((r >> 3) & 1);
@@ -227,7 +229,8 @@ struct Tile {
     typedef typename FragOf<T>::type frag;
 
     // Where a lane reads: what depends on the lane, once; everything else of an address is an exclusive-or or a sum with constants,
-    // since rows 16 apart have the same turn and units are numbered by bits.  (With addresses worked out per read, a step
+    // since rows 16 apart have the same turn and units are numbered by bits: those of a row's bytes, so tiles begin at whole rows in LDS,
+    // the kernel's dynamic memory at kTileAlign whatever static memory lies before it.  (With addresses worked out per read, a step
     // of the forward kernel for heads of 128 had 41 additions beside 32 reads, and their terms overflowed the registers.)
     struct Lane {
         uint32_t row, col;

@@ -22,7 +22,7 @@ constexpr int dq_keys() { return sizeof(T) * row_values(D) == 512 ? kKeyTile / 2
 template <typename T, int D, bool VEC>
 __global__ __launch_bounds__(256, sizeof(T) * row_values(D) == 512 ? 1 : 2) void attention_dq_kernel(AttnArgs a)
 {
-    extern __shared__ __attribute__((aligned(16))) char smem[];
+    extern __shared__ __attribute__((aligned(kTileAlign))) char smem[];
     typedef Tile<T, row_values(D)> tile;
     constexpr int kKeys = dq_keys<T, D>(), kTileBytes = kKeys * tile::kRowBytes;
     const int tid = threadIdx.x, lane = tid & 63, half = lane >> 5, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -187,7 +187,7 @@ constexpr int dkv_queries() { return D > 64 ? 32 : kKeyTile; }
 template <typename T, int D, bool VEC>
 __global__ __launch_bounds__(256, sizeof(T) * row_values(D) == 512 ? 1 : 2) void attention_dkv_kernel(AttnArgs a)
 {
-    extern __shared__ __attribute__((aligned(16))) char smem[];
+    extern __shared__ __attribute__((aligned(kTileAlign))) char smem[];
     typedef Tile<T, row_values(D)> tile;
     constexpr int kQueries = dkv_queries<D>(), kTileBytes = kQueries * tile::kRowBytes;
     constexpr bool kValuesInLds = D > 64;

@@ -110,7 +110,7 @@ __device__ __forceinline__ float log_sum(float m, float l) { return l == 0.0f ? 
 template <typename T, int D, bool VEC>
 __global__ __launch_bounds__(256, sizeof(T) * row_values(D) == 512 ? 1 : 2) void attention_forward_kernel(AttnArgs a)
 {
-    extern __shared__ __attribute__((aligned(16))) char smem[];
+    extern __shared__ __attribute__((aligned(kTileAlign))) char smem[];
     typedef Tile<T, row_values(D)> tile;
     constexpr int kTileBytes = kKeyTile * tile::kRowBytes;
     const int tid = threadIdx.x, lane = tid & 63, half = lane >> 5, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -235,7 +235,7 @@ template <typename T, int D> struct FewLayout {
 template <typename T, int D, bool VEC>
 __global__ __launch_bounds__(256) void attention_few_kernel(AttnArgs a)
 {
-    extern __shared__ __attribute__((aligned(16))) char smem[];
+    extern __shared__ __attribute__((aligned(kTileAlign))) char smem[];
     typedef FewLayout<T, D> L;
     __shared__ float stat[2][4][kFewRows];
     const int tid = threadIdx.x, lane = tid & 63, half = lane >> 5, wave = __builtin_amdgcn_readfirstlane(tid >> 6);

@@ -72,7 +72,7 @@ template <typename T, int WAVES> struct OnePass {
 template <typename T, int D, bool VEC, int WAVES>
 __global__ __launch_bounds__(64 * WAVES, 2) void attention_one_pass_kernel(AttnArgs a)
 {
-    extern __shared__ __attribute__((aligned(16))) char smem[];
+    extern __shared__ __attribute__((aligned(kTileAlign))) char smem[];
     typedef OnePass<T, WAVES> L;
     typedef typename L::tile tile;
     constexpr int kQueries = L::kQueries, kTileBytes = L::kTileBytes, kThreads = 64 * WAVES;
