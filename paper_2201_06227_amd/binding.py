@@ -751,13 +751,11 @@ def _same_device(*tensors: Optional[torch.Tensor]) -> int:
     return dev
 
 
-def _no_graph(*tensors: Optional[torch.Tensor]):
+def _refuse_graph():
     """The calls below record nothing for autograd: a tensor that wants a gradient through them would silently get none."""
     if torch.is_grad_enabled():
-        for t in tensors:
-            if t is not None and t.requires_grad:
-                raise ValueError("a result would have no autograd graph: call this under torch.no_grad() or with detached tensors "
-                                 "(the gradient is attention_backward's, position_bias_backward's)")
+        raise ValueError("a result would have no autograd graph: call this under torch.no_grad() or with detached tensors "
+                         "(the gradient is attention_backward's, position_bias_backward's)")
 
 
 def _heads(t: torch.Tensor) -> bytes:
@@ -768,12 +766,6 @@ def _heads(t: torch.Tensor) -> bytes:
     if sf != 1 and t.shape[3] > 1:
         raise ValueError("contiguous features expected")
     return _heads_struct.pack(t.data_ptr(), sb, st, sh)
-
-
-def _like(t: torch.Tensor) -> torch.Tensor:
-    """An output like t, laid out as t is (1.1 us; torch.empty of its shape 2.3); where t's elements overlap that may leave the features apart."""
-    out = torch.empty_like(t)
-    return out if out.stride(3) == 1 or out.shape[3] < 2 else torch.empty(t.shape, dtype=t.dtype, device=t.device)
 
 
 def _lens(t: Optional[torch.Tensor], batch: int) -> int:
@@ -833,12 +825,15 @@ def attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, causal: bool = 
     """egeria_attention: q [batch, q_len, heads, dim], k and v [batch, k_len, kv_heads, dim] (any strides with contiguous
     features) -> out like q, and lse fp32 [batch, heads, q_len].  scale: 1 / sqrt(dim) if not given.  No autograd: the gradient is
     attention_backward's, and tensors that require one are refused unless in torch.no_grad()."""
-    _no_graph(q, k, v, None if bias is None else bias.table)
+    if q.requires_grad or k.requires_grad or v.requires_grad or (bias is not None and bias.table.requires_grad):
+        _refuse_graph()
     dev = _same_device(q, k, v, q_lens, k_lens, out, lse, ws, None if bias is None else bias.table)
     desc, sizes, _tab = _attention_desc(q, k, v, causal, scale, q_lens, k_lens, bias)
     batch, q_len, heads, _ = q.shape
     if out is None:
-        out = _like(q)
+        out = torch.empty_like(q)                        # (1.1 us; torch.empty of its shape 2.3)
+        if out.stride(3) != 1:                           # q's elements overlap: that may take the features apart
+            out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
     elif out.shape != q.shape or out.dtype != q.dtype:
         raise ValueError("out must have q's shape and dtype")
     if lse is None:
@@ -846,8 +841,11 @@ def attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, causal: bool = 
     elif lse.shape != (batch, heads, q_len) or lse.dtype != torch.float32 or not lse.is_contiguous():
         raise ValueError("lse must be a contiguous fp32 tensor [batch, heads, q_len]")
     if ws is None:
-        ws = torch.empty(_attention_workspace_bytes(desc, sizes, 0), dtype=torch.uint8, device=q.device)
-    rc = _raw("egeria_attention", 9)(desc, _heads(q), _heads(k), _heads(v), _heads(out), lse.data_ptr(), ws.data_ptr(), _room(ws),
+        room = _attention_workspace_bytes(desc, sizes, 0)
+        ws = torch.empty(room, dtype=torch.uint8, device=q.device)
+    else:
+        room = _room(ws)
+    rc = _raw("egeria_attention", 9)(desc, _heads(q), _heads(k), _heads(v), _heads(out), lse.data_ptr(), ws.data_ptr(), room,
                                      torch._C._cuda_getCurrentRawStream(dev))
     if rc:
         _check(rc, "egeria_attention")
@@ -862,7 +860,8 @@ def attention_backward(dout: torch.Tensor, q: torch.Tensor, k: torch.Tensor, v: 
     """egeria_attention_backward: (dq, dk, dv, dtable) from the arguments and results of attention().  dtable is fp32
     [buckets, heads], or None without bias or with table_grad = False.  dq, dk, dv: tensors to write, e.g. the slices of a packed
     gradient.  No gradient of the gradient: a dout that requires one is refused unless in torch.no_grad()."""
-    _no_graph(dout)
+    if dout.requires_grad:
+        _refuse_graph()
     dev = _same_device(dout, q, k, v, out, lse, q_lens, k_lens, dq, dk, dv, ws, None if bias is None else bias.table)
     desc, sizes, _tab = _attention_desc(q, k, v, causal, scale, q_lens, k_lens, bias)
     if dout.shape != q.shape or dout.dtype != q.dtype or out.shape != q.shape or out.dtype != q.dtype:
@@ -873,16 +872,21 @@ def attention_backward(dout: torch.Tensor, q: torch.Tensor, k: torch.Tensor, v: 
     grads = []
     for g, t in ((dq, q), (dk, k), (dv, v)):
         if g is None:
-            g = _like(t)
+            g = torch.empty_like(t)
+            if g.stride(3) != 1:
+                g = torch.empty(t.shape, dtype=t.dtype, device=t.device)
         elif g.shape != t.shape or g.dtype != t.dtype:
             raise ValueError("dq, dk and dv must have the shapes and dtype of q, k and v")
         grads.append(g)
     dtable = torch.empty_like(bias.table) if bias is not None and table_grad else None
     if ws is None:
-        ws = torch.empty(_attention_workspace_bytes(desc, sizes, 1), dtype=torch.uint8, device=q.device)
+        room = _attention_workspace_bytes(desc, sizes, 1)
+        ws = torch.empty(room, dtype=torch.uint8, device=q.device)
+    else:
+        room = _room(ws)
     rc = _raw("egeria_attention_backward", 14)(
         desc, _heads(dout), _heads(q), _heads(k), _heads(v), _heads(out), lse.data_ptr(), _heads(grads[0]), _heads(grads[1]),
-        _heads(grads[2]), None if dtable is None else dtable.data_ptr(), ws.data_ptr(), _room(ws), torch._C._cuda_getCurrentRawStream(dev))
+        _heads(grads[2]), None if dtable is None else dtable.data_ptr(), ws.data_ptr(), room, torch._C._cuda_getCurrentRawStream(dev))
     if rc:
         _check(rc, "egeria_attention_backward")
     return (*grads, dtable)
@@ -892,7 +896,8 @@ def position_bias(bias: PositionBias, q_len: int, k_len: int, offset: int = 0, d
                   out: Optional[torch.Tensor] = None) -> torch.Tensor:
     """egeria_position_bias: [heads, q_len, k_len] of table entries; offset = position of query 0 among the keys.  A table that
     requires a gradient is refused unless in torch.no_grad()."""
-    _no_graph(bias.table)
+    if bias.table.requires_grad:
+        _refuse_graph()
     _same_device(bias.table, out)
     tab, heads = bias.c_struct(), bias.table.shape[1]
     if out is None:
@@ -907,7 +912,8 @@ def position_bias(bias: PositionBias, q_len: int, k_len: int, offset: int = 0, d
 def position_bias_backward(dbias: torch.Tensor, bias: PositionBias, offset: int = 0, ws: Optional[torch.Tensor] = None) -> torch.Tensor:
     """egeria_position_bias_backward: the gradient [buckets, heads] of bias.table from dbias [batch, heads, q_len, k_len] (or
     [heads, q_len, k_len])."""
-    _no_graph(dbias)
+    if dbias.requires_grad:
+        _refuse_graph()
     _same_device(dbias, bias.table, ws)
     tab, heads = bias.c_struct(), bias.table.shape[1]
     if dbias.dim() not in (3, 4) or dbias.shape[-3] != heads:
