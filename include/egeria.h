@@ -564,7 +564,8 @@ size_t egeria_attention_workspace_bytes(const egeria_attention_desc *desc, int32
  * misaligned pointer, a negative stride, an output whose elements overlap;
  * EGERIA_ERR_UNSUPPORTED for head_dim > 128, heads > 65535, lengths beyond 2^29,
  * tensors beyond 2^62 bytes, or a launch beyond 2^32 threads (2^24 tiles of 128
- * rows); EGERIA_ERR_WORKSPACE_TOO_SMALL. */
+ * rows; backward with 129 to 256 keys and heads of at most 64, 2^23 key heads);
+ * EGERIA_ERR_WORKSPACE_TOO_SMALL. */
 egeria_status egeria_attention(const egeria_attention_desc *desc, const egeria_heads *q, const egeria_heads *k,
                                const egeria_heads *v, const egeria_heads *out, float *lse, void *ws, size_t ws_bytes,
                                void *stream);

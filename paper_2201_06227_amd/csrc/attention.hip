@@ -257,7 +257,7 @@ egeria_status egeria_attention_backward(const egeria_attention_desc *desc, const
     if ((dtable && !desc->bias) || ((uintptr_t)dtable & 15u)) return EGERIA_ERR_INVALID_ARG;
     const Plan p = make_plan(desc, true);
     if (ws_bytes < p.total) return EGERIA_ERR_WORKSPACE_TOO_SMALL;
-    if (p.blocks * (p.one ? 512 : 256) > kMostThreads) return EGERIA_ERR_UNSUPPORTED;
+    if (p.blocks * (p.one && desc->k_len > 128 ? 512 : 256) > kMostThreads) return EGERIA_ERR_UNSUPPORTED;      // (a wave for 32 keys, four or eight of them)
     AttnArgs a = make_args(desc);
     a.d_o = view_of(dout), a.q = view_of(q), a.k = view_of(k), a.v = view_of(v), a.o = view_of(out);
     a.dq = view_of(dq), a.dk = view_of(dk), a.dv = view_of(dv);

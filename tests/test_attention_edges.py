@@ -207,3 +207,17 @@ def test_workspaces_that_are_smaller_than_they_look(eg, monkeypatch):  # noqa: F
     for call in (lambda: eg.attention(x, x, x, ws=ws), lambda: eg.attention_backward(x, x, x, x, x, lse, ws=ws), lambda: eg.position_bias_backward(torch.zeros(1, 2, 4, 4), pb, ws=ws)):
         with pytest.raises(ValueError, match="workspace"):
             call()
+
+
+@pytest.mark.gpu
+def test_eight_million_sequences(eg):  # noqa: F811
+    """2^23 workgroups of 256 threads are half of what a launch holds: sequences of one token, whose probability is 1."""
+    n = 1 << 23
+    q, k, v, dout = (torch.randn(n, 1, 1, 1, device=DEV, generator=torch.Generator(DEV).manual_seed(i)).bfloat16() for i in range(4))
+    out, lse = eg.attention(q, k, v)
+    assert torch.equal(out, v)
+    score = q.float() * k.float()                         # exact: two factors of 8 bits
+    assert ((lse.view(-1) - score.view(-1)).abs() <= 4 * 2.0 ** -24 * score.view(-1).abs()).all()      # to base 2 and back: two products and two constants
+    dq, dk, dv, _ = eg.attention_backward(dout, q, k, v, out, lse)
+    # p = 1 within the error of lse and of the exponent's two roundings, far below half a step of bf16 (2^-8): p is 1; ds = p (dout v - dout out) = 0
+    assert torch.equal(dv, dout) and not dq.any() and not dk.any()
