@@ -510,7 +510,11 @@ egeria_status egeria_cache_get(const egeria_cache_desc *desc, const void *cache,
  * Every element of every output is written: zeros for rows without a visible
  * pair, for queries at or beyond n_q and for keys at or beyond n_k.
  *
- * Scores, row statistics and sums are fp32.  With EGERIA_BF16, p and ds are
+ * Scores, row statistics and sums are fp32.  So a score's error is 2^-24 of what
+ * is added up in it, table entry included, and backward, a probability's is
+ * |L_i| 2^-23 of itself: numbers of 1e7 and more that all pairs of a row share
+ * leave nothing of their differences (pairs are hidden by the table's minus
+ * infinity, not by -1e9 for a whole row).  With EGERIA_BF16, p and ds are
  * rounded to bf16 where they enter the products on the matrix cores, and the
  * outputs once at the end; with EGERIA_F32 nothing is rounded below fp32.
  * Results do not depend on timing (no floating-point atomics between waves).

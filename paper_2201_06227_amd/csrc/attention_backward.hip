@@ -75,8 +75,9 @@ __global__ __launch_bounds__(256, sizeof(T) * row_values(D) == 512 ? 1 : 2) void
     float delta = (float)(sum + __shfl_xor(sum, 32));
     if (half == 0 && i < a.q_len && part == 0) a.delta[row] = delta;
     const float lse = i < nq ? a.lse[row] : -INFINITY;
-    // p 2^whole is what the exponential gives; its factor is in the difference that it is multiplied by
-    const float whole = lse == -INFINITY ? 0.0f : fminf(fmaxf(rintf(lse * kLog2e), -64.0f), 64.0f), by_p = __builtin_amdgcn_exp2f(-whole);
+    // p 2^whole is what the exponential gives; its factor is in the difference that it is multiplied by (none for rows without a pair and
+    // those whose log-sum-exp would swallow it)
+    const float whole = fabsf(lse) > kFine ? 0.0f : fminf(fmaxf(rintf(lse * kLog2e), -64.0f), 64.0f), by_p = __builtin_amdgcn_exp2f(-whole);
     const float base = lse == -INFINITY ? INFINITY : lowered(lse, whole), c = a.scale * kLog2e, sign = sign_of<typename tile::frag>(lane) * by_p;
     delta *= by_p;
     v16f dq[D / 32];

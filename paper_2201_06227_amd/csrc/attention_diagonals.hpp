@@ -18,8 +18,12 @@ __device__ __forceinline__ float sign_of(int index) { return sizeof(F) == 16 && 
 
 // Base-2 log-sum-exp of a row less a whole number, which the caller gives back as a power of two: exponents s c - L are rounded to the
 // precision of their own size, and that is log2 of the keys where scores are of size one.  (The product is exact inside the fma; the rest
-// is that of log2 e.)
-__device__ __forceinline__ float lowered(float lse, float whole) { return fmaf(lse, 1.92596303e-8f, fmaf(lse, kLog2e, -whole)); }
+// is that of log2 e.)  Beyond kFine that rest is less than the result's own rounding: the plain product, as the dk / dv kernel has it.
+constexpr float kFine = 65536.0f;
+__device__ __forceinline__ float lowered(float lse, float whole)
+{
+    return fabsf(lse) > kFine ? lse * kLog2e - whole : fmaf(lse, 1.92596303e-8f, fmaf(lse, kLog2e, -whole));
+}
 
 __device__ __forceinline__ float sum16(const v16f &s)
 {

@@ -221,3 +221,30 @@ def test_eight_million_sequences(eg):  # noqa: F811
     dq, dk, dv, _ = eg.attention_backward(dout, q, k, v, out, lse)
     # p = 1 within the error of lse and of the exponent's two roundings, far below half a step of bf16 (2^-8): p is 1; ds = p (dout v - dout out) = 0
     assert torch.equal(dv, dout) and not dq.any() and not dk.any()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("shape", [(2, 70, 200, 4, 4, 64), (64, 40, 70, 4, 4, 64), (64, 40, 200, 4, 4, 64)], ids=str)
+@pytest.mark.parametrize("offset", [-1e9, 1e9, -3e9, -1e10, 1e10, -9e29])
+def test_an_offset_of_a_whole_head(eg, dtype, shape, offset):  # noqa: F811
+    """A table entry that is large, but hides nothing, for all pairs of a head: an fp32 log-sum-exp has no bits left for its probabilities, but its
+    numbers stay finite, and the other heads' are what they are without it."""
+    tab = torch.randn(8, 4, generator=torch.Generator().manual_seed(6))
+    q, k, v, dout = make(dtype, *shape, seed=33)
+    run_and_check(eg, dtype, q, k, v, dout, bias=(tab, 20, True))
+    on = [t.to(DEV) for t in (q, k, v, dout)]
+    results = []
+    for x in (tab[:, 1].clone(), offset):
+        tab[:, 1] = x
+        pb = eg.PositionBias(tab.to(DEV), 20, True)
+        out, lse = eg.attention(*on[:3], bias=pb)
+        dq, dk, dv, dtable = eg.attention_backward(on[3], *on[:3], out, lse, bias=pb)
+        results.append((out, lse.transpose(1, 2), dq, dk, dv, dtable[:, :, None].transpose(0, 1)[None].transpose(1, 2)))
+    rest = [0, 2, 3]
+    for a, b in zip(*results):
+        assert torch.equal(a[:, :, rest], b[:, :, rest])
+    # scores of this head are below 6.5 in size, so p < 666 whatever part of them is left; |dP - D| < 2 * 64 * 25; at most 200 keys of size 5, scale 1/8
+    for name, t in zip(("out", "dq", "dk", "dv"), (results[1][n] for n in (0, 2, 3, 4))):
+        assert torch.isfinite(t).all() and t.abs().max() < 666 * 3200 * 200 * 5 / 8, name
+    assert torch.isfinite(results[1][5]).all()
