@@ -248,3 +248,147 @@ def test_an_offset_of_a_whole_head(eg, dtype, shape, offset):  # noqa: F811
     for name, t in zip(("out", "dq", "dk", "dv"), (results[1][n] for n in (0, 2, 3, 4))):
         assert torch.isfinite(t).all() and t.abs().max() < 666 * 3200 * 200 * 5 / 8, name
     assert torch.isfinite(results[1][5]).all()
+
+
+# Calls of at least 48 tiles of 128 queries, which go to the kernel for whole tiles whatever their keys are; several tiles of keys.
+TILES = [(4, 130, 200, 12, 4, 96), (4, 130, 600, 12, 12, 128), (4, 130, 330, 12, 6, 127), (2, 257, 520, 9, 3, 128), (4, 129, 641, 12, 3, 64), (8, 140, 300, 6, 2, 33)]
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("shape", TILES, ids=lambda s: "x".join(map(str, s)))
+@pytest.mark.parametrize("kind", ["plain", "causal", "bias", "causal bias lengths"])
+def test_whole_tiles(eg, dtype, shape, kind):  # noqa: F811
+    b, nq, nk, h = shape[:4]
+    bias = (torch.randn(32, h, generator=torch.Generator().manual_seed(7)), 128, "causal" not in kind) if "bias" in kind else None
+    rng = np.random.default_rng(nk)
+    lens = dict(q_lens=[nq, *rng.integers(1, nq + 1, b - 1).tolist()], k_lens=[nk, *rng.integers(1, nk + 1, b - 1).tolist()]) if "lengths" in kind else {}
+    run_and_check(eg, dtype, *make(dtype, *shape, seed=nk), causal="causal" in kind, bias=bias, **lens)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("shape", [(4, 130, 330, 12, 4, 128), (64, 70, 40, 4, 2, 64), (64, 40, 200, 4, 2, 33)], ids=str)
+@pytest.mark.parametrize("causal", [False, True])
+def test_padding_of_large_calls_is_not_read(eg, dtype, shape, causal):  # noqa: F811
+    """What lies behind a sequence's length, NaN and infinity among it, in the kernel for whole tiles and the backward pass of few keys."""
+    b, nq, nk = shape[:3]
+    q, k, v, dout = make(dtype, *shape, seed=41)
+    rng = np.random.default_rng(b)
+    ql, kl = rng.integers(0, nq + 1, b).tolist(), rng.integers(0, nk + 1, b).tolist()
+    want = run_and_check(eg, dtype, q, k, v, dout, causal=causal, q_lens=ql, k_lens=kl)
+    for i in range(b):
+        for t, n in ((q, ql[i]), (dout, ql[i]), (k, kl[i]), (v, kl[i])):
+            t[i, n:] = math.nan
+        k[i, kl[i]::2] = math.inf
+    lens = [torch.tensor(n, dtype=torch.int32, device=DEV) for n in (ql, kl)]
+    q, k, v, dout = (t.to(DEV) for t in (q, k, v, dout))
+    out, lse = eg.attention(q, k, v, causal=causal, q_lens=lens[0], k_lens=lens[1])
+    got = (out, lse, *eg.attention_backward(dout, q, k, v, out, lse, causal=causal, q_lens=lens[0], k_lens=lens[1])[:3])
+    for a, w in zip(got, want):
+        assert torch.equal(a, w)
+
+
+def whole(rng, *shape, most=1):
+    """Whole numbers in [-most, most], none of them 0."""
+    x = torch.randint(1, most + 1, shape, generator=rng) * (2 * torch.randint(0, 2, shape, generator=rng) - 1)
+    return x.double()
+
+
+COUNTS = {**WAYS, "heads of 128": (2, 140, 300, 16, 4, 128), "odd rows": (2, 70, 300, 4, 2, 75), "few keys": (64, 70, 100, 4, 2, 64), "keys of eight waves": (33, 90, 256, 4, 4, 40),
+          "short": (2, 33, 65, 2, 1, 16)}
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("way", COUNTS)
+@pytest.mark.parametrize("causal", [False, True])
+def test_every_pair_counts_once(eg, dtype, way, causal):  # noqa: F811
+    """All scores 0 (queries, or keys, of 0), whole numbers elsewhere: out is a mean of whole numbers and every gradient a sum of whole numbers over a
+    number of keys, so that one pair too few or too many shows where a bound for ordinary numbers would let it pass.
+    Bounds: p is 1 in the forward pass, exactly; sums of whole numbers are exact; a division and a product are left, 2 u.  Backward, L = log n < 9 with
+    4 roundings and the exponent's: p is off by less than (5 * 9 + 16) u < 2^-18 of itself, a sum of n terms by n u; bf16 rounds p where it enters a
+    product, by 2^-8 of itself at most and not at all where n is a power of two, which the lengths are without the causal mask."""
+    b, nq, nk, h, g, d = COUNTS[way]
+    rng = torch.Generator().manual_seed(51)
+    lens = [1 << (nk.bit_length() - 1 - i % 4) for i in range(b)]
+    ql = [nq - i % 3 for i in range(b)]
+    kl, qls = (torch.tensor(n, dtype=torch.int32, device=DEV) for n in (lens, ql))
+    v, dout = whole(rng, b, nk, g, d, most=8), whole(rng, b, nq, h, d)
+    tab = torch.zeros(16, h)
+    u, half, operand = 2.0 ** -24, *STEPS[dtype]
+    if not causal:
+        operand = 0.0
+    zero_k = dict(q=whole(rng, b, nq, h, d, most=4), k=torch.zeros(b, nk, g, d).double())
+    zero_q = dict(q=torch.zeros(b, nq, h, d).double(), k=whole(rng, b, nk, g, d, most=4))
+    for x in (zero_k, zero_q):
+        on = [t.to(T[dtype]).to(DEV) for t in (x["q"], x["k"], v)]
+        pb = eg.PositionBias(tab.to(DEV), 40, not causal)
+        out, lse = eg.attention(*on, causal=causal, q_lens=qls, k_lens=kl, scale=0.5, bias=pb)
+        bare = eg.attention(*on, causal=causal, q_lens=qls, k_lens=kl, scale=0.5)[0]
+        # the gradients' own inputs: values of 1 and -1 and a saved output of 0, so that dS is a whole number <= d over a number of keys
+        ones = torch.sign(v)
+        saved = torch.zeros_like(out)
+        grads = eg.attention_backward(dout.to(T[dtype]).to(DEV), *on[:2], ones.to(T[dtype]).to(DEV), saved, lse, causal=causal, q_lens=qls, k_lens=kl, scale=0.5, bias=pb)
+        want, bound = [np.zeros(s.shape) for s in (x["q"], x["q"], x["k"], x["k"], tab)], [np.zeros(s.shape) for s in (x["q"], x["q"], x["k"], x["k"], tab)]
+        for i in range(b):
+            n, m = ql[i], lens[i]
+            shift = m - n if causal else 0
+            seen = (np.arange(m)[None] <= np.arange(n)[:, None] + shift) if causal else np.ones((n, m), bool)
+            p = seen / np.maximum(seen.sum(1, keepdims=True), 1)
+            grid = ao.bucket_grid(n, m, shift, 16, 40, not causal)
+            for j in range(h):
+                e = j // (h // g)
+                vv, ov, do, qq, kk = (np64(t) for t in (v[i, :m, e], ones[i, :m, e], dout[i, :n, j], x["q"][i, :n, j], x["k"][i, :m, e]))
+                want[0][i, :n, j] = (seen @ vv) / np.maximum(seen.sum(1, keepdims=True), 1)        # (the sum first: it is whole)
+                bound[0][i, :n, j] = (half + 2 * u) * np.abs(want[0][i, :n, j])
+                ds = p * (do @ ov.T)
+                rel = 2.0 ** -18 + operand
+                want[1][i, :n, j] = 0.5 * ds @ kk
+                bound[1][i, :n, j] = 0.5 * np.abs(ds) @ np.abs(kk) * (rel + m * u)
+                want[2][i, :m, e] += 0.5 * ds.T @ qq
+                bound[2][i, :m, e] += 0.5 * np.abs(ds).T @ np.abs(qq) * (rel + n * h // g * u)
+                want[3][i, :m, e] += p.T @ do
+                bound[3][i, :m, e] += p.T @ np.abs(do) * (rel + n * h // g * u)
+                want[4][:, j] += np.bincount(grid.ravel(), weights=ds.ravel(), minlength=16)
+                bound[4][:, j] += np.bincount(grid.ravel(), weights=np.abs(ds).ravel(), minlength=16) * (2.0 ** -18 + (n + m) * u)
+        for at in (1, 2, 3):
+            bound[at] += half * np.abs(want[at])
+        close(out, want[0], bound[0], "out")
+        assert torch.equal(out, bare)
+        for name, t, w, e in zip(("dq", "dk", "dv", "dtable"), grads, want[1:], bound[1:]):
+            close(t, w, e, name)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("shape", [(3, 1, 301, 2051), (5, 3, 77, 77), (1, 1, 1201, 1301), (7, 2, 33, 4099), (2, 3, 130, 2048), (40, 1, 9, 1), (1, 1, 1, 1), (2, 2, 260, 264), (9, 1, 8, 8195)], ids=str)
+@pytest.mark.parametrize("offset,buckets,far,both", [(0, 32, 128, True), (7, 2, 2, False), (100, 128, 1000, False)])
+def test_every_bias_gradient_counts_once(eg, dtype, shape, offset, buckets, far, both):  # noqa: F811
+    """Whole numbers up to 3, whose sums stay below 2^24: every partial sum is exact in fp32, so the result is."""
+    d = whole(torch.Generator().manual_seed(sum(shape)), *shape, most=3)
+    grad, size = ao.position_bias_backward(d.numpy(), buckets, offset, far, both)
+    assert size.max() < 2 ** 24
+    got = eg.position_bias_backward(d.to(T[dtype]).to(DEV), eg.PositionBias(torch.zeros(buckets, shape[1], device=DEV), far, both), offset=offset)
+    assert np.array_equal(np64(got), grad)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("shape", [(1, 16, 1100, 2101), (2, 4, 4110, 4128)], ids=str)
+def test_bias_of_many_columns_to_a_workgroup(eg, dtype, shape):  # noqa: F811
+    """Rows enough for workgroups that go through several pieces of the columns: the bias as a tensor, and whole numbers' sums, exactly."""
+    b, h, nq, nk = shape
+    offset, buckets, far = 50, 32, 128
+    rel = np.arange(-nq + 1 - offset, nk - offset)
+    by = np.array([ao.bucket_of(int(r), buckets, far, True) for r in rel])
+    grid = by[np.arange(nk)[None, :] - np.arange(nq)[:, None] + nq - 1]
+    tab = torch.randn(buckets, h, generator=torch.Generator().manual_seed(8))
+    pb = eg.PositionBias(tab.to(DEV), far, True)
+    got = eg.position_bias(pb, nq, nk, offset=offset, dtype=T[dtype])
+    want = tab.to(T[dtype]).to(DEV)[torch.from_numpy(grid).to(DEV)].permute(2, 0, 1)
+    assert torch.equal(got, want)
+    d = torch.randint(-1, 2, shape, generator=torch.Generator().manual_seed(9), dtype=torch.int8)
+    got = eg.position_bias_backward(d.to(DEV).to(T[dtype]), pb, offset=offset)
+    sums = np.stack([np.bincount(grid.ravel(), weights=d[:, k].sum(0, dtype=torch.int64).numpy().ravel(), minlength=buckets) for k in range(h)], 1)
+    assert np.abs(sums).max() < 2 ** 22 and np.array_equal(np64(got), sums)      # (partial sums of random signs: thousands, far below 2^24)
