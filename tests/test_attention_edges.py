@@ -392,3 +392,33 @@ def test_bias_of_many_columns_to_a_workgroup(eg, dtype, shape):  # noqa: F811
     got = eg.position_bias_backward(d.to(DEV).to(T[dtype]), pb, offset=offset)
     sums = np.stack([np.bincount(grid.ravel(), weights=d[:, k].sum(0, dtype=torch.int64).numpy().ravel(), minlength=buckets) for k in range(h)], 1)
     assert np.abs(sums).max() < 2 ** 22 and np.array_equal(np64(got), sums)      # (partial sums of random signs: thousands, far below 2^24)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("what,x", [("key", math.nan), ("value", math.nan), ("value", math.inf)])
+@pytest.mark.parametrize("shape", [(2, 70, 150, 4, 2, 64), (1, 150, 300, 4, 2, 128), (64, 20, 40, 4, 2, 32), (64, 70, 200, 4, 2, 64)], ids=str)
+def test_gradients_of_a_key_or_value_that_is_not_finite(eg, dtype, what, x, shape):  # noqa: F811
+    """No gradient of the heads that see it is finite, but dv beside a value (which it does not depend on); all others are as without it."""
+    q, k, v, dout = make(dtype, *shape, seed=26)
+    h, nk = shape[3], shape[2]
+    tab = torch.randn(8, h, generator=torch.Generator().manual_seed(4))
+    pb = eg.PositionBias(tab.to(DEV), 20, True)
+    scale = np.float64(np.float32(1.0 / math.sqrt(shape[5])))
+    out, lse = eg.attention(*(t.to(DEV) for t in (q, k, v)), bias=pb)
+    want = ao.attention(np64(q), np64(k), np64(v), scale, bias=(np64(tab), 20, True), dout=np64(dout), saved=(np64(out), np64(lse)), half_step=STEPS[dtype][0],
+                        operand_step=STEPS[dtype][1])
+    (k if what == "key" else v)[0, nk // 2, 1, 5] = x
+    on = [t.to(DEV) for t in (q, k, v)]
+    out, lse = eg.attention(*on, bias=pb)
+    dq, dk, dv, dtable = eg.attention_backward(dout.to(DEV), *on, out, lse, bias=pb)
+    heads = slice(h // 2, h)
+    for name, t, at in (("dq", dq, (0, slice(None), heads)), ("dk", dk, (0, slice(None), 1)), ("dv", dv, (0, slice(None), 1)), ("dtable", dtable, (slice(None), heads))):
+        if name == "dv" and what == "value":
+            at = None
+        elif name != "dtable":
+            assert not torch.isfinite(t[at]).any(), name
+        if at is not None:
+            t[at] = 0.0
+            want[name][at] = 0.0
+        close(t, want[name], want["bound"][name], name)
