@@ -222,13 +222,6 @@ __global__ __launch_bounds__(64 * WAVES, 2) void attention_one_pass_kernel(AttnA
                     for (int r = 0; r < 16; r += 4) {
                         const float4 base = *(const float4 *)&stat[kBuffer][0][32 * n + row_of(r, half)];
                         const float bs[4] = {base.x, base.y, base.z, base.w};
-                        // without a bias no addition of it, in workgroups of four waves (bf16 200 x 128 x 8 x 64 83 us, now 75; in those
-                        // of eight one more way gains nothing and costs calls with a bias 3 %: 64 x 256 x 12 x 64 98 us, 101.6)
-                        if (sizeof(T) == 2 && WAVES == 4 && !bias.on) {
-#pragma unroll
-                            for (int e = 0; e < 4; ++e) p[r + e] = __builtin_amdgcn_exp2f(fmaf(s[r + e], c, -bs[e]));
-                            continue;
-                        }
                         v4f_any t;
                         if (one) t = v4f_any(beta);
                         else t = bias.four(rel - row_of(r, 0) - 3);
