@@ -92,8 +92,10 @@ int64_t few_tiles(const egeria_attention_desc *d)
 
 // The forward kernel for few rows, and how many workgroups share a row tile's keys there (0: the other kernel).  A tile of 128 queries
 // leaves most of its waves without rows up to 32 queries; and where there are few such tiles, tiles of 32 rows and a share of the
-// keys for each wave occupy more of the device (128-row tiles / this way, us: fp32 2 x 512 x 6 x 64 40 / 20, bf16 1 x 1000 x 4 x 128 26 /
-// 20, 2 x 512 x 6 x 64 causal 14 / 14, 7 x 64 x 8 x 64 6 / 7, 1 x 2048 x 3 x 128 46 / 51).  Splits have at least 256 keys.
+// keys for each wave occupy more of the device.  The border lies between what was measured, 128-row tiles / this way, us: below 48 tiles
+// fp32 1 x 512 x 6 x 64 39 / 16, 1 x 130 x 8 x 128 36 / 19, bf16 1 x 1000 x 4 x 128 26 / 18, but 2 x 512 x 5 x 64 12.4 / 15.2; with 48
+// bf16 1 x 2048 x 3 x 128 46 / 50, 2 x 512 x 6 x 64 causal 13.0 / 14.8, but fp32 2 x 512 x 6 x 64 39 / 18.  Splits have at least 256
+// keys.
 int few_splits(const egeria_attention_desc *d)
 {
     const int64_t blocks = (int64_t)d->batch * d->heads * (((int64_t)d->q_len + kRowTile - 1) / kRowTile);
@@ -132,7 +134,8 @@ int parts_of(int64_t blocks, int64_t steps, int64_t slots, double more, bool cau
 }
 
 // The backward kernel that makes everything in one pass: where its keys and LDS fit and a workgroup for each key head of the batch
-// gives half the compute units work.
+// gives half the compute units work (two kernels / this one, us: fp32 24 x 197 x 12 x 64 180 / 124, bf16 200 x 128 x 8 x 64 78 / 64; at 130 x
+// 100 x 4 x 32 causal 22 / 23).
 bool one_pass(const egeria_attention_desc *d)
 {
     return d->k_len <= kOnePassKeys && d->head_dim <= 64 && (int64_t)d->batch * d->kv_heads >= 128 && one_pass_lds(d, true) <= kMostLds;

@@ -212,7 +212,7 @@ __device__ __forceinline__ int row_of(int r, int half) { return 8 * (r >> 2) + 4
 // transposed by the read itself for bf16).  A row is kept in units of 16 bytes, unit u of row r at slot u ^ turn(r).  The 64 banks
 // of 4 bytes hold 256 bytes, i.e. 16 units: the 16 rows that a quarter of a wave reads a unit of have 16 different (row, slot) places
 // if turn() takes different values over the rows that share a place; and of the four rows that half a wave reads 4 units of each
-// across, those that share places have turn() differ in the bits above the lowest two.  Rows of 128 bytes (two to a line of banks): the
+// across (col_frag; other ways across a tile may have conflicts), those that share places have turn() differ in the bits above the lowest two.  Rows of 128 bytes (two to a line of banks): the
 // bits of r / 2 in reverse; longer rows: r with its lowest two bits on top.
 constexpr int kTileAlign = 512;             // of LDS that holds tiles: a whole number of rows (Lane)
 template <typename T, int D>
