@@ -422,3 +422,13 @@ def test_gradients_of_a_key_or_value_that_is_not_finite(eg, dtype, what, x, shap
             t[at] = 0.0
             want[name][at] = 0.0
         close(t, want[name], want["bound"][name], name)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("shape,causal", [((1, 1, 700, 64, 1, 128), True), ((1, 1, 700, 33, 1, 128), False), ((2, 3, 200, 64, 2, 64), False), ((1, 200, 900, 4, 2, 128), False),
+                                          ((4, 130, 400, 12, 3, 96), False), ((130, 40, 200, 2, 1, 64), False), ((64, 30, 100, 2, 2, 32), True)], ids=str)
+def test_the_largest_tables(eg, dtype, shape, causal):  # noqa: F811
+    """128 buckets up to distances beyond 900 on both sides, and up to 64 query heads to a key head: the most LDS that a call takes."""
+    run_and_check(eg, dtype, *make(dtype, *shape, seed=61), causal=causal, bias=(torch.randn(128, shape[3], generator=torch.Generator().manual_seed(9)), 1024, True))
+    run_and_check(eg, dtype, *make(dtype, *shape, seed=62), causal=causal, bias=(torch.randn(127, shape[3], generator=torch.Generator().manual_seed(10)), 1024, False))
