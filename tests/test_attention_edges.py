@@ -432,3 +432,70 @@ def test_the_largest_tables(eg, dtype, shape, causal):  # noqa: F811
     """128 buckets up to distances beyond 900 on both sides, and up to 64 query heads to a key head: the most LDS that a call takes."""
     run_and_check(eg, dtype, *make(dtype, *shape, seed=61), causal=causal, bias=(torch.randn(128, shape[3], generator=torch.Generator().manual_seed(9)), 1024, True))
     run_and_check(eg, dtype, *make(dtype, *shape, seed=62), causal=causal, bias=(torch.randn(127, shape[3], generator=torch.Generator().manual_seed(10)), 1024, False))
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("kw", [dict(b=4, s=48, hidden=128, heads=4, ffn=256, n_layers=2), dict(b=3, s=33, hidden=96, heads=3, ffn=160, n_layers=1)], ids=str)
+def test_training_and_scoring_of_encoder_layers(eg, orc, kw):  # noqa: F811
+    """An encoder in training whose attention is this one, and the evaluation of its layers: the activations that the training forward leaves are scored
+    against the int8 reference of a snapshot of the same layers, before and after a step along the gradients."""
+    import torch.nn.functional as F
+
+    import synth_inputs as si
+    from paper_2201_06227_amd.evaluator import PlasticityEvaluator
+    wl = si.make_bert(seed=77, train_act_dtype="f32", **kw)
+    hid, nh, n_layers = kw["hidden"], kw["heads"], kw["n_layers"]
+
+    class Attention(torch.autograd.Function):
+        @staticmethod
+        def forward(ctx, qkv):
+            out, lse = eg.attention(*qkv.unbind(2))
+            ctx.save_for_backward(qkv, out, lse)
+            return out
+
+        @staticmethod
+        def backward(ctx, dout):
+            qkv, out, lse = ctx.saved_tensors
+            dqkv = torch.empty_like(qkv)
+            eg.attention_backward(dout, *qkv.unbind(2), out, lse, dq=dqkv[:, :, 0], dk=dqkv[:, :, 1], dv=dqkv[:, :, 2])
+            return dqkv
+
+    def plain(qkv):
+        q, k, v = (t.transpose(1, 2) for t in qkv.unbind(2))
+        return (torch.softmax(q @ k.transpose(2, 3) / math.sqrt(hid // nh), -1) @ v).transpose(1, 2)
+
+    def forward(x, weights, attend):
+        acts = []
+        for l in range(n_layers):
+            wq, wo, w1, w2 = weights[4 * l:4 * l + 4]
+            b, s = x.shape[:2]
+            y = F.layer_norm(x + attend(F.linear(x, wq).view(b, s, 3, nh, hid // nh)).reshape(b, s, hid) @ wo.t(), (hid,), eps=1e-12)
+            x = F.layer_norm(y + F.linear(F.gelu(F.linear(y, w1)), w2), (hid,), eps=1e-12)
+            acts.append(x)
+        return acts
+
+    x, target = torch.from_numpy(wl.x), torch.randn(wl.x.shape, generator=torch.Generator().manual_seed(1))
+
+    def run(dtype, dev, attend):
+        w = [torch.from_numpy(t).to(dev, dtype).requires_grad_() for t in wl.train_weights]
+        acts = forward(x.to(dev, dtype), w, attend)
+        (0.5 * (acts[-1] - target.to(dev, dtype)).square().sum()).backward()
+        return w, acts
+
+    w, acts = run(torch.float32, DEV, Attention.apply)
+    w64, acts64 = run(torch.float64, "cpu", plain)
+    # fp32 sums of at most 288 terms, a dozen one behind the other: 12 * 290 u = 2e-4 of the terms' size, and terms that cancel to a fifth of it
+    for a, b in zip([*acts, *(t.grad for t in w)], [*acts64, *(t.grad for t in w64)]):
+        a, b = a.detach().double().cpu(), b.detach()
+        assert (a - b).norm() <= 1e-3 * b.norm()
+    ev = PlasticityEvaluator(wl.kind, wl.dims, [torch.from_numpy(t).to(DEV) for t in wl.weights], [None] * len(wl.weights), device=DEV)
+    wl.biases = [None] * len(wl.weights)
+    a_ref = orc.ref_forward(wl)["a_ref"]
+    with torch.no_grad():
+        stepped = forward(x.to(DEV), [t - 1e-3 * t.grad for t in w], lambda qkv: eg.attention(*qkv.unbind(2))[0])
+    for hooked in (acts, stepped):
+        a_t = [a.detach().reshape(a.shape[0], -1).contiguous() for a in hooked]
+        p = ev.step(x.to(DEV), a_t).cpu().numpy()
+        for l, t in enumerate(a_t):
+            want = orc.sp_loss(t.cpu().numpy(), a_ref[l].reshape(t.shape))
+            assert abs(p[l] - want) <= 1e-4 * abs(want) + 1e-12 * 4.0 / kw["b"], l
