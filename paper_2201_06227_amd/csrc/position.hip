@@ -113,7 +113,7 @@ __global__ __launch_bounds__(256) void position_bias_backward_kernel(Buckets b, 
     const int i0 = (int)rb * deal.rows + (int)(threadIdx.x >> deal.lg) * kRows;
     const int last = (int)rb * deal.rows + deal.rows < q_len ? (int)rb * deal.rows + deal.rows : q_len;
     const int64_t total = batch * heads * q_len * (int64_t)k_len;
-    float left = 0.0f, right = 0.0f;                               // patches whose distances all lie beyond the table
+    double left = 0.0, right = 0.0;                                // distances beyond the table: long sums, of values that may cancel
     const int hi = b.both ? b.far : 0;
     for (int c = 0; c < deal.cols; ++c) {
         const int j0 = (int)(((cb * deal.cols + c) << deal.lg) + (threadIdx.x & ((1 << deal.lg) - 1))) * N;
@@ -157,9 +157,9 @@ __global__ __launch_bounds__(256) void position_bias_backward_kernel(Buckets b, 
             }
         const int first = j0 - (i0 + kRows - 1) - offset;
         if (first >= hi || first + kRows + N - 2 <= -b.far) {
-            float s = 0.0f;
+            double s = 0.0;
 #pragma unroll
-            for (int e = 0; e < kRows + N - 1; ++e) s += d[e];
+            for (int e = 0; e < kRows + N - 1; ++e) s += (double)d[e];
             if (first >= hi) right += s;
             else left += s;
         } else {
@@ -167,8 +167,8 @@ __global__ __launch_bounds__(256) void position_bias_backward_kernel(Buckets b, 
             for (int e = 0; e < kRows + N - 1; ++e) {
                 const int rel = first + e;
                 // entries inside the table are different in every lane of the half; what lies beyond its ends is the lane's own sum
-                if (rel <= -b.far) left += d[e];
-                else if (rel >= hi) right += d[e];
+                if (rel <= -b.far) left += (double)d[e];
+                else if (rel >= hi) right += (double)d[e];
                 else mine[rel + b.far] += d[e];
                 asm volatile("" ::: "memory");                  // the next entry is another lane's: no read of it before this write
             }
@@ -179,8 +179,8 @@ __global__ __launch_bounds__(256) void position_bias_backward_kernel(Buckets b, 
     right = wave_sum(right);
     wave_lds_turn();
     if ((threadIdx.x & 63) == 0) {
-        mine[0] += left;                                           // the ends of the table have the same buckets as what lies beyond
-        mine[entries - 1] += right;
+        mine[0] += (float)left;                                    // the ends of the table have the same buckets as what lies beyond
+        mine[entries - 1] += (float)right;
     }
     const int64_t part = ((int64_t)sh * deal.row_blocks + rb) * deal.col_blocks + cb, parts = (int64_t)deal.shares * deal.row_blocks * deal.col_blocks;
     bucket_sums(spans, sums, 8, entries, entries, rows_of_table, partials + ((int64_t)h * parts + part) * rows_of_table);

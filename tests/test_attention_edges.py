@@ -499,3 +499,17 @@ def test_training_and_scoring_of_encoder_layers(eg, orc, kw):  # noqa: F811
         for l, t in enumerate(a_t):
             want = orc.sp_loss(t.cpu().numpy(), a_ref[l].reshape(t.shape))
             assert abs(p[l] - want) <= 1e-4 * abs(want) + 1e-12 * 4.0 / kw["b"], l
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("offset", [-5000, 5000])
+def test_far_sums_that_cancel(eg, dtype, offset):  # noqa: F811
+    """Score gradients beyond the table, all of one bucket, whose large parts cancel next to each other: what is left is the sum, not the rounding of fp32."""
+    d = torch.zeros(2, 3, 64, 640)
+    d[:, :, ::8, 0::8], d[:, :, ::8, 1::8], d[:, :, ::8, 2::8] = 2.0 ** 25, 1.0, -2.0 ** 25
+    pb = eg.PositionBias(torch.zeros(32, 3, device=DEV), 128, True)
+    got = eg.position_bias_backward(d.to(T[dtype]).to(DEV), pb, offset=offset)
+    want = torch.zeros(32, 3)
+    want[31 if offset < 0 else 15] = 2 * 8 * 80
+    assert torch.equal(got.cpu(), want)
